@@ -404,6 +404,84 @@ hbp_status hbp_packed_ce(const void* logits, int64_t logit_stride_t, int32_t tot
                          int32_t normalizer, float t_ave, void* dlogits_or_null, float* loss_out,
                          float* token_loss_or_null, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- token embedding of a packed buffer ------------------------------------------------------------ */
+
+enum { HBP_BF16 = 0, HBP_F32 = 1 }; /* element types */
+
+typedef struct {
+  int32_t total_tokens; /* T, at most 2^24                                                        */
+  int32_t vocab, dim;   /* table [vocab, dim]; any width from 1 to 2^24                           */
+  int32_t table_type;   /* HBP_BF16 or HBP_F32: the table and its gradient                        */
+  int32_t row_type;     /* HBP_BF16 or HBP_F32: the looked-up rows and their gradient             */
+  float scale;          /* s, any finite value                                                    */
+  int64_t table_stride, row_stride; /* elements from row to row; 0 = dim.  At least dim, no other alignment */
+} hbp_embed_desc;
+
+/*
+ * hbp_embed_fwd — rows of the embedding table for the tokens of a packed buffer.
+ *
+ *   rows[t,:] = scale * table[tokens[t],:]      computed in fp32, rounded once to row_type
+ *
+ * A token outside [0, vocab) (padding, say -1) gives a row of zeros, as such a label gives no loss in hbp_packed_ce.
+ * table, tokens (int32 [T]), rows: DEVICE, each aligned to its element.  total_tokens = 0: no-op.  Columns between dim and
+ * row_stride are left untouched.
+ * Errors: INVALID_ARG (null or misaligned pointers, negative sizes, vocab or dim < 1, a scale that is not finite, a bad
+ * type), SHAPE (a stride below dim), UNSUPPORTED (dim or total_tokens above 2^24, vocab of INT32_MAX), DEVICE.
+ */
+hbp_status hbp_embed_fwd(const hbp_embed_desc* desc, const void* table, const int32_t* tokens, void* rows, void* stream);
+
+/* Bytes of device workspace hbp_embed_bwd needs (256-byte aligned base): the sorted tokens and, fp32, the parts of sums
+ * that cross a chunk of sorted tokens.  Never more for fewer tokens. */
+hbp_status hbp_embed_bwd_workspace_bytes(const hbp_embed_desc* desc, size_t* bytes_out);
+
+/*
+ * hbp_embed_bwd — gradient of the table.
+ *
+ *   d_table[v,:]  =  scale * sum_{t: tokens[t] = v} d_rows[t,:]     accumulate = 0: every row is written, zeros where no
+ *                                                                   token has its id
+ *   d_table[v,:] +=  the same                                       accumulate = 1: only rows with a token are touched
+ *                                                                   (the gradient of a tied output projection, or of
+ *                                                                   earlier micro-batches, is in d_table already)
+ *
+ * Sums are fp32 over the tokens in a fixed order (no atomics: the same call gives the same bits) and rounded once, with
+ * what d_table held, to table_type.  Tokens outside [0, vocab) contribute nothing.  Columns between dim and
+ * table_stride are left untouched.  Same placement, alignment and errors as the lookup, and WORKSPACE.
+ * total_tokens = 0: zeros d_table, or a no-op where it accumulates.
+ */
+hbp_status hbp_embed_bwd(const hbp_embed_desc* desc, const void* d_rows, const int32_t* tokens, int32_t accumulate,
+                         void* d_table, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- gradient norm over many tensors, and clipping -------------------------------------------------- */
+
+/* Bytes of device workspace hbp_grad_sumsq needs (256-byte aligned base). */
+hbp_status hbp_grad_workspace_bytes(int32_t n_tensors, size_t* bytes_out);
+
+/*
+ * hbp_grad_sumsq — *sumsq = (accumulate ? *sumsq : 0) + sum of the squares of all elements of all tensors, in 64 bits.
+ *
+ * tensors[n_tensors] (DEVICE pointers), sizes[n_tensors] (elements; 0 allowed) and types[n_tensors] (HBP_BF16, HBP_F32)
+ * are HOST arrays, read before the call returns (they travel as kernel arguments: a captured call keeps its list, and
+ * nothing is copied or allocated on the device).  Every tensor is contiguous and aligned to its element, nothing more.
+ * sumsq: DEVICE, one double.  Between this call and hbp_grad_clip a data-parallel caller whose ranks hold different
+ * gradients (sharded ones) adds *sumsq up over its ranks.  The order of the additions depends on the sizes alone.
+ * Errors: INVALID_ARG (null or misaligned pointers, negative sizes, a bad type or flag), UNSUPPORTED (a tensor above 2^40
+ * elements), WORKSPACE, NO_MEMORY (host), DEVICE.
+ */
+hbp_status hbp_grad_sumsq(const void* const* tensors, const int64_t* sizes, const int32_t* types, int32_t n_tensors,
+                          int32_t accumulate, double* sumsq, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * hbp_grad_clip — outs[i] = tensors[i] * (max_norm / norm) where norm = sqrt(*sumsq) is above max_norm, else tensors[i].
+ *
+ * outs_or_null = NULL, or outs[i] = tensors[i]: in place; gradients under the limit are then not touched.  An element is
+ * multiplied in fp32 and rounded once to its tensor's type.  Where the norm is infinite or no number, nothing is scaled:
+ * the caller reads *norm_out_or_null (DEVICE, one float) and skips the step.  max_norm: 0 or more, infinity allowed.
+ * Errors as above, and INVALID_ARG for a max_norm that is negative or no number, and where a tensor that is written
+ * overlaps another one that is read or written (the same tensor listed twice would be scaled twice).
+ */
+hbp_status hbp_grad_clip(const void* const* tensors, void* const* outs_or_null, const int64_t* sizes, const int32_t* types,
+                         int32_t n_tensors, const double* sumsq, float max_norm, float* norm_out_or_null, void* stream);
+
 /*
  * hbp_mfma_probe — measurement aid: the second denominator of the roofline.  Launches, on `stream`,
  * one kernel in which every SIMD of `n_cu` compute units (two wavefronts each) issues nothing but

@@ -17,7 +17,9 @@ HBP_TILES_QUERY, HBP_TILES_KEY = 0, 1
 EXPORTED_SYMBOLS = ["hbp_status_string", "hbp_pack_plan", "hbp_order_query_tiles", "hbp_tile_rows", "hbp_fwd_tile_rows", "hbp_workspace_bytes",
                     "hbp_profile_capacity", "hbp_varlen_attn_fwd", "hbp_varlen_attn_bwd", "hbp_varlen_attn_bwd_static",
                     "hbp_set_kernel_events", "hbp_mfma_probe", "hbp_balance_packing",
-                    "hbp_packed_ce_workspace_bytes", "hbp_packed_ce", "hbp_auto_select"]
+                    "hbp_packed_ce_workspace_bytes", "hbp_packed_ce", "hbp_auto_select",
+                    "hbp_embed_fwd", "hbp_embed_bwd_workspace_bytes", "hbp_embed_bwd",
+                    "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip"]
 
 # numpy views of hbp_pack / hbp_batch
 PACK_DTYPE = np.dtype([("level", "<i4"), ("first_item", "<i4"), ("n_items", "<i4"), ("n_tokens", "<i4"),
@@ -68,6 +70,13 @@ class AttnDesc(ctypes.Structure):
                 ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
                 ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
                 ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64)]
+
+
+class EmbedDesc(ctypes.Structure):
+    """Mirror of ``hbp_embed_desc``."""
+    _fields_ = [("total_tokens", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("table_type", ctypes.c_int32), ("row_type", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("table_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
 def library_path() -> str:
@@ -126,6 +135,19 @@ def load_library():
     lib.hbp_mfma_probe.argtypes = [i32, i32, vp, vp]
     lib.hbp_auto_select.restype = i32
     lib.hbp_auto_select.argtypes = [vp, i32, vp, i32, i32, i32, ctypes.POINTER(Profile), vp, vp, i32p, i32p]
+    embedp, sizep = ctypes.POINTER(EmbedDesc), ctypes.POINTER(ctypes.c_size_t)
+    lib.hbp_embed_fwd.restype = i32
+    lib.hbp_embed_fwd.argtypes = [embedp, vp, vp, vp, vp]
+    lib.hbp_embed_bwd_workspace_bytes.restype = i32
+    lib.hbp_embed_bwd_workspace_bytes.argtypes = [embedp, sizep]
+    lib.hbp_embed_bwd.restype = i32
+    lib.hbp_embed_bwd.argtypes = [embedp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.hbp_grad_workspace_bytes.restype = i32
+    lib.hbp_grad_workspace_bytes.argtypes = [i32, sizep]
+    lib.hbp_grad_sumsq.restype = i32
+    lib.hbp_grad_sumsq.argtypes = [vp, vp, vp, i32, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.hbp_grad_clip.restype = i32
+    lib.hbp_grad_clip.argtypes = [vp, vp, vp, vp, i32, vp, ctypes.c_float, vp, vp]
     _lib = lib
     return lib
 
@@ -343,6 +365,75 @@ def hbp_packed_ce(logits, logit_stride_t: int, total_tokens: int, vocab: int, la
                                       _ptr(stream))
     if st != 0:
         raise HbpError(st, "hbp_packed_ce")
+
+
+HBP_BF16, HBP_F32 = 0, 1
+
+
+def hbp_embed_fwd(desc: EmbedDesc, table, tokens, rows, stream: Optional[int] = None) -> None:
+    """Enqueue the lookup of a packed buffer's tokens; see include/hbp.h."""
+    st = load_library().hbp_embed_fwd(ctypes.byref(desc), _ptr(table), _ptr(tokens), _ptr(rows), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_embed_fwd")
+
+
+def hbp_embed_bwd_workspace_bytes(desc: EmbedDesc) -> int:
+    out = ctypes.c_size_t()
+    st = load_library().hbp_embed_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(out))
+    if st != 0:
+        raise HbpError(st, "hbp_embed_bwd_workspace_bytes")
+    return int(out.value)
+
+
+def hbp_embed_bwd(desc: EmbedDesc, d_rows, tokens, accumulate: bool, d_table, workspace,
+                  stream: Optional[int] = None) -> None:
+    """Enqueue the gradient of the embedding table."""
+    st = load_library().hbp_embed_bwd(ctypes.byref(desc), _ptr(d_rows), _ptr(tokens), int(accumulate), _ptr(d_table),
+                                      _ptr(workspace), 0 if workspace is None else _nbytes(workspace), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_embed_bwd")
+
+
+class GradList:
+    """Host arrays of hbp_grad_sumsq and hbp_grad_clip: addresses, element counts and types (HBP_BF16, HBP_F32)."""
+
+    def __init__(self, addresses: Sequence[int], sizes: Sequence[int], types: Sequence[int],
+                 outs: Optional[Sequence[int]] = None):
+        self.n = len(addresses)
+        if len(sizes) != self.n or len(types) != self.n or (outs is not None and len(outs) != self.n):
+            raise HbpError(1, "GradList")
+        self.addresses = np.array(addresses, dtype=np.uint64)
+        self.sizes = np.array(sizes, dtype=np.int64)
+        self.types = np.array(types, dtype=np.int32)
+        self.outs = None if outs is None else np.array(outs, dtype=np.uint64)
+        at = lambda a: a.ctypes.data if a is not None and a.size else None
+        self.args = (at(self.addresses), at(self.sizes), at(self.types), at(self.outs))
+
+
+def hbp_grad_workspace_bytes(n_tensors: int) -> int:
+    out = ctypes.c_size_t()
+    st = load_library().hbp_grad_workspace_bytes(int(n_tensors), ctypes.byref(out))
+    if st != 0:
+        raise HbpError(st, "hbp_grad_workspace_bytes")
+    return int(out.value)
+
+
+def hbp_grad_sumsq(grads: GradList, accumulate: bool, sumsq, workspace, stream: Optional[int] = None) -> None:
+    """Enqueue the sum of squares of all tensors' elements into ``sumsq`` (one double on the device)."""
+    tensors, sizes, types, _ = grads.args
+    st = load_library().hbp_grad_sumsq(tensors, sizes, types, grads.n, int(accumulate), _ptr(sumsq), _ptr(workspace),
+                                       0 if workspace is None else _nbytes(workspace), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_grad_sumsq")
+
+
+def hbp_grad_clip(grads: GradList, sumsq, max_norm: float, norm_out=None, stream: Optional[int] = None) -> None:
+    """Enqueue the clipping of all tensors to ``max_norm``, given the sum of squares."""
+    tensors, sizes, types, outs = grads.args
+    st = load_library().hbp_grad_clip(tensors, outs, sizes, types, grads.n, _ptr(sumsq), float(max_norm),
+                                      _ptr(norm_out), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_grad_clip")
 
 
 def hbp_mfma_probe(n_cu: int, mfma_per_wave: int, sink, stream=None) -> None:

@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libhbp.so")
 LIB_RACE_HUNT = os.path.join(PKG, "libhbp_racehunt.so")   # the same library with a full fence after every phase
 OBJ_DIR = os.path.join(PKG, "_build")
-SOURCES = ["api.hip", "fwd.hip", "bwd.hip", "loss.hip", "plan.cpp", "balance.cpp", "auto_select.cpp"]
+SOURCES = ["api.hip", "api_step.hip", "fwd.hip", "bwd.hip", "loss.hip", "embed.hip", "grads.hip", "plan.cpp", "balance.cpp", "auto_select.cpp"]
 
 HIP_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-munsafe-fp-atomics", "-Wno-inline-asm",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

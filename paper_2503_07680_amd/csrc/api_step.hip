@@ -1,0 +1,189 @@
+// C ABI of the operators around a pack's attention and loss: argument validation on the host, then kernel launches on the
+// caller's stream.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "rows.hpp"
+
+namespace {
+
+constexpr int32_t kMaxDim = 1 << 24, kMaxTokens = 1 << 24;
+
+int type_bytes(int32_t type) { return type == HBP_BF16 ? 2 : type == HBP_F32 ? 4 : 0; }
+bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
+
+hbp_status check_embed(const hbp_embed_desc* d, hbp::EmbedParams* p) {
+  if (!d) return HBP_ERR_INVALID_ARG;
+  if (d->total_tokens < 0 || d->vocab < 1 || d->dim < 1 || !std::isfinite(d->scale)) return HBP_ERR_INVALID_ARG;
+  if (!type_bytes(d->table_type) || !type_bytes(d->row_type)) return HBP_ERR_INVALID_ARG;
+  if (d->dim > kMaxDim || d->total_tokens > kMaxTokens || d->vocab == INT32_MAX) return HBP_ERR_UNSUPPORTED;
+  p->T = d->total_tokens;
+  p->V = d->vocab;
+  p->dim = d->dim;
+  p->table_st = d->table_stride ? d->table_stride : d->dim;
+  p->row_st = d->row_stride ? d->row_stride : d->dim;
+  p->scale = d->scale;
+  if (p->table_st < d->dim || p->row_st < d->dim) return HBP_ERR_SHAPE;
+  return HBP_OK;
+}
+
+// The tensors that have elements, in the batches of the launches; false: bad arguments.
+hbp_status grad_batches(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n,
+                        std::vector<hbp::GradBatch>& batches) {
+  if (n < 0 || (n > 0 && (!in || !sizes || !types))) return HBP_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n; ++i) {
+    if (sizes[i] < 0 || !type_bytes(types[i])) return HBP_ERR_INVALID_ARG;
+    if (sizes[i] == 0) continue;
+    if (sizes[i] > ((int64_t)1 << 40)) return HBP_ERR_UNSUPPORTED;
+    const int es = type_bytes(types[i]);
+    if (!in[i] || !aligned_to(in[i], es) || (out && (!out[i] || !aligned_to(out[i], es)))) return HBP_ERR_INVALID_ARG;
+    const uint64_t chunks = (uint64_t)(sizes[i] + hbp::kGradChunk - 1) / hbp::kGradChunk;
+    if (batches.empty() || batches.back().n == hbp::kGradBatch || batches.back().first_chunk[batches.back().n] + chunks > INT32_MAX) {
+      batches.emplace_back();
+      batches.back().n = 0;
+      batches.back().first_chunk[0] = 0;
+    }
+    hbp::GradBatch& b = batches.back();
+    b.in[b.n] = in[i];
+    b.out[b.n] = out ? out[i] : const_cast<void*>(in[i]);
+    b.size[b.n] = sizes[i];
+    b.type[b.n] = (uint8_t)types[i];
+    b.first_chunk[b.n + 1] = b.first_chunk[b.n] + (uint32_t)chunks;
+    ++b.n;
+  }
+  return HBP_OK;
+}
+int groups_of(const hbp::GradBatch& b) { return (int)std::min<uint32_t>(b.first_chunk[b.n], hbp::kGradMaxGroups); }
+
+// Whether what is written overlaps anything else that is written, or anything read but the same tensor at the same place.
+bool overlaps(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n) {
+  struct Range {
+    uintptr_t from, to;
+    int32_t i;
+    bool written;
+  };
+  std::vector<Range> r;
+  r.reserve(2 * (size_t)n);
+  for (int32_t i = 0; i < n; ++i) {
+    if (sizes[i] == 0) continue;
+    const uintptr_t bytes = (uintptr_t)sizes[i] * type_bytes(types[i]), a = (uintptr_t)in[i], b = out ? (uintptr_t)out[i] : a;
+    r.push_back({b, b + bytes, i, true});
+    if (a != b) r.push_back({a, a + bytes, i, false});
+  }
+  std::sort(r.begin(), r.end(), [](const Range& x, const Range& y) { return x.from < y.from; });
+  // two ranges that overlap, one of them written
+  uintptr_t end_written = 0, end_any = 0;
+  for (const Range& x : r) {
+    if (x.from < end_written || (x.written && x.from < end_any)) return true;
+    end_any = std::max(end_any, x.to);
+    if (x.written) end_written = std::max(end_written, x.to);
+  }
+  return false;
+}
+
+}  // namespace
+
+extern "C" hbp_status hbp_embed_fwd(const hbp_embed_desc* desc, const void* table, const int32_t* tokens, void* rows, void* stream) {
+  hbp::EmbedParams p;
+  const hbp_status st = check_embed(desc, &p);
+  if (st != HBP_OK) return st;
+  if (p.T == 0) return HBP_OK;
+  if (!table || !tokens || !rows) return HBP_ERR_INVALID_ARG;
+  if (!aligned_to(table, type_bytes(desc->table_type)) || !aligned_to(rows, type_bytes(desc->row_type)) || !aligned_to(tokens, 4))
+    return HBP_ERR_INVALID_ARG;
+  p.tokens = tokens;
+  return hbp::launch_embed_fwd(p, desc->table_type, desc->row_type, table, rows, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
+}
+
+extern "C" hbp_status hbp_embed_bwd_workspace_bytes(const hbp_embed_desc* desc, size_t* bytes_out) {
+  if (!bytes_out) return HBP_ERR_INVALID_ARG;
+  hbp::EmbedParams p;
+  const hbp_status st = check_embed(desc, &p);
+  if (st != HBP_OK) return st;
+  *bytes_out = hbp::embed_bwd_layout(p.T, p.V, p.dim).total;
+  return HBP_OK;
+}
+
+extern "C" hbp_status hbp_embed_bwd(const hbp_embed_desc* desc, const void* d_rows, const int32_t* tokens, int32_t accumulate,
+                                    void* d_table, void* workspace, size_t workspace_bytes, void* stream) {
+  hbp::EmbedParams p;
+  const hbp_status st = check_embed(desc, &p);
+  if (st != HBP_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return HBP_ERR_INVALID_ARG;
+  if (p.T > 0 && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < hbp::embed_bwd_layout(p.T, p.V, p.dim).total))
+    return HBP_ERR_WORKSPACE;
+  if (p.T == 0 && accumulate) return HBP_OK;
+  if (!d_table || (p.T > 0 && (!d_rows || !tokens))) return HBP_ERR_INVALID_ARG;
+  if (!aligned_to(d_table, type_bytes(desc->table_type)) || !aligned_to(d_rows, type_bytes(desc->row_type)) || !aligned_to(tokens, 4))
+    return HBP_ERR_INVALID_ARG;
+  p.tokens = tokens;
+  return hbp::launch_embed_bwd(p, desc->table_type, desc->row_type, d_rows, d_table, accumulate != 0, static_cast<char*>(workspace),
+                               static_cast<hipStream_t>(stream))
+             ? HBP_ERR_DEVICE
+             : HBP_OK;
+}
+
+extern "C" hbp_status hbp_grad_workspace_bytes(int32_t n_tensors, size_t* bytes_out) {
+  if (!bytes_out || n_tensors < 0) return HBP_ERR_INVALID_ARG;
+  // a batch ends at kGradBatch tensors, or where its chunks fill 31 bits: at most one more a tensor of 2^40 elements
+  *bytes_out = ((size_t)n_tensors / hbp::kGradBatch + 1) * hbp::kGradMaxGroups * sizeof(double);
+  return HBP_OK;
+}
+
+extern "C" hbp_status hbp_grad_sumsq(const void* const* tensors, const int64_t* sizes, const int32_t* types, int32_t n_tensors,
+                                     int32_t accumulate, double* sumsq, void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    if (n_tensors < 0 || !sumsq || !aligned_to(sumsq, 8) || (accumulate != 0 && accumulate != 1)) return HBP_ERR_INVALID_ARG;
+    std::vector<hbp::GradBatch> batches;
+    const hbp_status st = grad_batches(tensors, nullptr, sizes, types, n_tensors, batches);
+    if (st != HBP_OK) return st;
+    size_t partials = 0;
+    for (const auto& b : batches) partials += groups_of(b);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < partials * sizeof(double)) return HBP_ERR_WORKSPACE;
+    double* partial = static_cast<double*>(workspace);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    int at = 0;
+    for (const auto& b : batches) {
+      if (hbp::launch_grad_sumsq(b, groups_of(b), partial + at, s) != 0) return HBP_ERR_DEVICE;
+      at += groups_of(b);
+    }
+    return hbp::launch_grad_total(partial, at, sumsq, accumulate != 0, s) ? HBP_ERR_DEVICE : HBP_OK;
+  } catch (const std::bad_alloc&) {
+    return HBP_ERR_NO_MEMORY;
+  } catch (...) {
+    return HBP_ERR_INVALID_ARG;
+  }
+}
+
+extern "C" hbp_status hbp_grad_clip(const void* const* tensors, void* const* outs_or_null, const int64_t* sizes, const int32_t* types,
+                                    int32_t n_tensors, const double* sumsq, float max_norm, float* norm_out_or_null, void* stream) {
+  try {
+    if (n_tensors < 0 || !sumsq || !aligned_to(sumsq, 8) || !(max_norm >= 0.f)) return HBP_ERR_INVALID_ARG;
+    std::vector<hbp::GradBatch> batches;
+    const hbp_status st = grad_batches(tensors, outs_or_null, sizes, types, n_tensors, batches);
+    if (st != HBP_OK) return st;
+    if (overlaps(tensors, outs_or_null, sizes, types, n_tensors)) return HBP_ERR_INVALID_ARG;
+    if (batches.empty()) {
+      batches.emplace_back();
+      batches.back().n = 0;
+      batches.back().first_chunk[0] = 0;
+    }
+    bool in_place = true;
+    for (const auto& b : batches)
+      for (int i = 0; i < b.n; ++i) in_place = in_place && b.in[i] == b.out[i];
+    for (size_t i = 0; i < batches.size(); ++i) {
+      const auto& b = batches[i];
+      if (hbp::launch_grad_clip(b, std::max(1, groups_of(b)), sumsq, max_norm, in_place, i ? nullptr : norm_out_or_null,
+                                static_cast<hipStream_t>(stream)) != 0)
+        return HBP_ERR_DEVICE;
+    }
+    return HBP_OK;
+  } catch (const std::bad_alloc&) {
+    return HBP_ERR_NO_MEMORY;
+  } catch (...) {
+    return HBP_ERR_INVALID_ARG;
+  }
+}

@@ -1,0 +1,532 @@
+// Token embedding of a packed buffer and its gradient, gfx950.
+//
+//   lookup     Y[t] = s W[x_t], zeros where x_t is no token (negative, or the vocabulary's size and beyond)
+//   gradient   dW[v] (+)= s sum over t with x_t = v, in ascending t, of dY[t]
+//
+// Both move bytes and compute next to nothing.  The gradient works on the tokens sorted by id, equal ids in the order of
+// their positions, so that every row of dW is summed in one fixed order, in 32 bits, and written once, without atomics:
+// (1) a stable radix sort of (id, position), nine bits of the id a pass; (2) the sorted positions are cut into chunks of a
+// fixed number, whatever the ids, so that a frequent id costs no workgroup more than the others: a run of equal ids inside a
+// chunk is summed and written, of one that goes beyond it the chunk's part is kept; (3) the parts of such runs are added up
+// in the chunks' order.  A fresh dW is zeroed beside the sort, which leaves the chip idle otherwise.
+#include "rows.hpp"
+
+namespace hbp {
+
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kOneTile = 16384;              // tokens that one workgroup sorts by itself
+constexpr int kTileRounds = 4, kTile = kTileRounds * kSortThreads;  // of each workgroup where there are more
+constexpr int kSmallChunks = 16384;          // up to so many tokens: chunks of 16, else of 32
+constexpr uint32_t kNoKey = 0xffffffffu;
+
+int log2_threads_per_row(int n_vec) {  // 64 to 256: a wavefront is always on one row
+  return n_vec > 128 ? 8 : n_vec > 64 ? 7 : 6;
+}
+int n_vectors(int dim) { return dim >= 8 ? (dim + 7) / 8 : dim; }
+int key_bits(int32_t V) { return 32 - __builtin_clz((uint32_t)V); }  // ids 0 .. V - 1, and V for "no token"
+
+// A thread's share of a row: VEC values from column col on, of which the first `skip` belong to the thread before (the last
+// eight of a row whose width is no multiple of eight).
+struct Span {
+  int col, skip;
+};
+template <int VEC>
+__device__ __forceinline__ Span span_of(int v, int dim) {
+  const int col = VEC == 8 ? min(8 * v, dim - 8) : v;
+  return {col, VEC * v - col};
+}
+template <int TYPE, int VEC>
+__device__ __forceinline__ f32x8_row load_span(const typename RowType<TYPE>::T* p) {
+  if constexpr (VEC == 8) return RowType<TYPE>::widen(RowType<TYPE>::load_raw(p));
+  f32x8_row x = {};
+  x[0] = RowType<TYPE>::load1(p);
+  return x;
+}
+
+// ------------------------------------------------------------------------------------- lookup
+// A workgroup takes U rows a pass with its rows' loads under way together.
+template <int TABLE, int ROW, int VEC, int U>
+__global__ __launch_bounds__(kRowThreads) void embed_lookup_kernel(EmbedParams p, const typename RowType<TABLE>::T* table,
+                                                                   typename RowType<ROW>::T* out, int log2_tpr) {
+  const int tpr = 1 << log2_tpr, per_pass = kRowThreads >> log2_tpr;
+  const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> log2_tpr);
+  const int64_t row0 = (int64_t)blockIdx.x * (per_pass * U) + sub;
+  int id[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t r = row0 + (int64_t)u * per_pass;
+    id[u] = r < p.T ? p.tokens[r] : -1;
+  }
+  const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
+  for (int v = threadIdx.x & (tpr - 1); v < n_vec; v += tpr) {
+    const int col = span_of<VEC>(v, p.dim).col;
+    f32x8_row x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      x[u] = f32x8_row{};
+      if (id[u] >= 0 && id[u] < p.V) x[u] = load_span<TABLE, VEC>(table + (int64_t)id[u] * p.table_st + col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = row0 + (int64_t)u * per_pass;
+      if (r >= p.T) break;
+      auto* to = out + r * p.row_st + col;
+      const f32x8_row y = x[u] * p.scale;
+      if constexpr (VEC == 8) RowType<ROW>::store(to, y);
+      else RowType<ROW>::store1(to, y[0]);
+    }
+  }
+}
+
+// --------------------------------------------------------------------------------------- sort
+typedef volatile __attribute__((address_space(3))) uint32_t* LdsCounts;
+
+// One tile of up to E * 1024 elements, element (wave * rounds + e) * 64 + lane in key[e] of a thread (kNoKey: none).  Counts
+// the digit `shift` of its elements into counts[digit][wave] and returns in rank[e] how many of the same digit the wavefront
+// has in front of each.  counts start as zeros.
+template <int E>
+__device__ __forceinline__ void wave_ranks(const uint32_t (&key)[E], uint32_t (&rank)[E], int rounds, int shift, LdsCounts counts) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (e >= rounds) continue;
+    const bool is = key[e] != kNoKey;
+    const uint32_t d = (key[e] >> shift) & (kDigits - 1);
+    uint64_t same = __builtin_amdgcn_ballot_w64(is);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+      const bool one = (d >> b) & 1;
+      const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
+      same &= one ? ones : ~ones;
+    }
+    rank[e] = 0;
+    if (is) {  // LDS operations of a wavefront are in order: all read the count before the first of each digit raises it
+      const uint32_t before = counts[d * kSortWaves + wave];
+      const uint32_t in_front = (uint32_t)__popcll(same & below);
+      __builtin_amdgcn_wave_barrier();
+      if (in_front == 0) counts[d * kSortWaves + wave] = before + (uint32_t)__popcll(same);
+      __builtin_amdgcn_wave_barrier();
+      rank[e] = before + in_front;
+    }
+  }
+}
+// exclusive sum over the workgroup of one value a thread; sums: one word a wavefront
+__device__ __forceinline__ uint32_t before_me(uint32_t x, uint32_t* sums) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint32_t s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(s, d, 64);
+    if (lane >= d) s += y;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = s;
+  __syncthreads();
+  uint32_t base = 0;
+  for (int w = 0; w < wave; ++w) base += sums[w];
+  return base + s - x;
+}
+// counts[digit][wave] -> the tile's elements of smaller digits, and of the same one in the wavefronts before
+__device__ __forceinline__ void scan_counts(uint32_t* counts, uint32_t* sums) {
+  constexpr int N = kDigits * kSortWaves / kSortThreads;
+  uint32_t c[N], total = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    c[i] = counts[threadIdx.x * N + i];
+    total += c[i];
+  }
+  uint32_t at = before_me(total, sums);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    counts[threadIdx.x * N + i] = at;
+    at += c[i];
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void clear_counts(uint32_t* counts) {
+  for (int i = threadIdx.x; i < kDigits * kSortWaves; i += kSortThreads) counts[i] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ uint32_t key_of(int32_t token, int32_t V) { return token >= 0 && token < V ? (uint32_t)token : (uint32_t)V; }
+
+// Zeros into rows [V part / parts, V (part + 1) / parts) of dW, by the workgroups from `first` on; a wavefront a row.
+struct Fill {
+  char* table;
+  int64_t stride_bytes, row_bytes;
+  int32_t V, part, parts, blocks;  // blocks: 0 for none
+};
+__device__ __forceinline__ void fill_rows(const Fill& f, int block) {
+  const int lane = threadIdx.x & 63;
+  const int64_t waves = (int64_t)f.blocks * kSortWaves, wave = (int64_t)block * kSortWaves + (threadIdx.x >> 6);
+  const int64_t from = (int64_t)f.V * f.part / f.parts, to = (int64_t)f.V * (f.part + 1) / f.parts;
+  for (int64_t r = from + wave; r < to; r += waves) {
+    char* row = f.table + r * f.stride_bytes;
+    int64_t b = lane * 16;
+    for (; b + 16 <= f.row_bytes; b += 1024) __builtin_nontemporal_store(u32x4_any{0, 0, 0, 0}, (u32x4_any*)(row + b));
+    // at most one piece of the row's end is left, to one lane; rows are whole elements of 2 or 4 bytes
+    if (b < f.row_bytes)
+      for (; b < f.row_bytes; b += 2) *(uint16_t*)(row + b) = 0;
+  }
+}
+
+// T <= kOneTile: the first workgroup sorts in LDS, the others zero dW.
+template <int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_one_kernel(const int32_t* tokens, int T, int V, int bits, uint32_t* keys,
+                                                                      uint32_t* order, Fill fill) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  if (blockIdx.x > 0) {
+    fill_rows(fill, blockIdx.x - 1);
+    return;
+  }
+  constexpr int N = ROUNDS * kSortThreads;
+  uint32_t* const counts = lds;
+  uint32_t* const sums = lds + kDigits * kSortWaves;
+  uint32_t* const key_lds = sums + kSortWaves;
+  uint16_t* const pos_lds = (uint16_t*)(key_lds + N);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, rounds = (T + kSortThreads - 1) / kSortThreads;
+  uint32_t key[ROUNDS], rank[ROUNDS];
+  uint32_t pos[ROUNDS];
+#pragma unroll
+  for (int e = 0; e < ROUNDS; ++e) {
+    const int i = (wave * rounds + e) * 64 + lane;
+    const bool is = e < rounds && i < T;
+    key[e] = is ? key_of(tokens[is ? i : 0], V) : kNoKey;
+    pos[e] = i;
+  }
+  for (int shift = 0; shift < bits; shift += kDigitBits) {
+    clear_counts(counts);
+    wave_ranks<ROUNDS>(key, rank, rounds, shift, (LdsCounts)counts);
+    __syncthreads();
+    scan_counts(counts, sums);
+    const bool last = shift + kDigitBits >= bits;
+#pragma unroll
+    for (int e = 0; e < ROUNDS; ++e) {
+      if (e >= rounds || key[e] == kNoKey) continue;
+      const uint32_t to = counts[((key[e] >> shift) & (kDigits - 1)) * kSortWaves + wave] + rank[e];
+      key_lds[to] = key[e];
+      pos_lds[to] = (uint16_t)pos[e];
+    }
+    __syncthreads();
+    if (last) {
+      for (int i = threadIdx.x; i < T; i += kSortThreads) {
+        keys[i] = key_lds[i];
+        order[i] = pos_lds[i];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < ROUNDS; ++e) {
+        const int i = (wave * rounds + e) * 64 + lane;
+        const bool is = e < rounds && i < T;
+        key[e] = is ? key_lds[i] : kNoKey;
+        pos[e] = is ? pos_lds[i] : 0;
+      }
+    }
+    // clear_counts has a barrier in front of the next pass's scatter
+  }
+}
+template <int ROUNDS>
+constexpr int sort_one_lds() {
+  return (kDigits * kSortWaves + kSortWaves) * 4 + ROUNDS * kSortThreads * 6;
+}
+
+// More tokens: a workgroup a tile.  counts[tile][digit] of one pass; first pass: the keys are the tokens.
+__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(const int32_t* tokens, const uint32_t* keys, int T, int V, int shift,
+                                                                   int tiles, uint32_t* counts, Fill fill) {
+  __shared__ uint32_t c[kDigits];
+  if ((int)blockIdx.x >= tiles) {
+    fill_rows(fill, blockIdx.x - tiles);
+    return;
+  }
+  if (threadIdx.x < kDigits) c[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kTileRounds; ++e) {
+    const int64_t i = (int64_t)blockIdx.x * kTile + e * kSortThreads + threadIdx.x;
+    if (i < T) {
+      const uint32_t k = keys ? keys[i] : key_of(tokens[i], V);
+      atomicAdd(&c[(k >> shift) & (kDigits - 1)], 1u);  // whole numbers: the order does not matter
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < kDigits) counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = c[threadIdx.x];
+}
+__global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(const int32_t* tokens, const uint32_t* keys, const uint32_t* order,
+                                                                     int T, int V, int shift, int tiles, const uint32_t* tile_counts,
+                                                                     uint32_t* keys_out, uint32_t* order_out, Fill fill) {
+  __shared__ uint32_t counts[kDigits * kSortWaves];
+  __shared__ uint32_t sums[kSortWaves], start[kDigits], total[2][kDigits], earlier[2][kDigits];
+  if ((int)blockIdx.x >= tiles) {
+    fill_rows(fill, blockIdx.x - tiles);
+    return;
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint32_t key[kTileRounds], pos[kTileRounds], rank[kTileRounds];
+#pragma unroll
+  for (int e = 0; e < kTileRounds; ++e) {
+    const int64_t i = (int64_t)blockIdx.x * kTile + (wave * kTileRounds + e) * 64 + lane;
+    key[e] = kNoKey;
+    pos[e] = (uint32_t)i;
+    if (i < T) {
+      key[e] = keys ? keys[i] : key_of(tokens[i], V);
+      if (order) pos[e] = order[i];
+    }
+  }
+  clear_counts(counts);
+  // a digit's elements in the tiles before this one, and in all (half of the threads take every second tile)
+  {
+    const int d = threadIdx.x & (kDigits - 1), half = threadIdx.x >> kDigitBits;
+    uint32_t all = 0, before = 0;
+    for (int t = half; t < tiles; t += 2) {
+      const uint32_t x = tile_counts[(int64_t)t * kDigits + d];
+      all += x;
+      if (t < (int)blockIdx.x) before += x;
+    }
+    total[half][d] = all;
+    earlier[half][d] = before;
+  }
+  wave_ranks<kTileRounds>(key, rank, kTileRounds, shift, (LdsCounts)counts);
+  __syncthreads();
+  scan_counts(counts, sums);
+  {
+    const int d = threadIdx.x & (kDigits - 1);
+    const uint32_t all = threadIdx.x < kDigits ? total[0][d] + total[1][d] : 0;
+    const uint32_t smaller = before_me(all, sums);
+    // a digit's first place, less what scan_counts has in front of it in this tile
+    if (threadIdx.x < kDigits) start[d] = smaller + earlier[0][d] + earlier[1][d] - counts[d * kSortWaves];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kTileRounds; ++e) {
+    if (key[e] == kNoKey) continue;
+    const uint32_t d = (key[e] >> shift) & (kDigits - 1), to = start[d] + counts[d * kSortWaves + wave] + rank[e];
+    keys_out[to] = key[e];
+    order_out[to] = pos[e];
+  }
+}
+
+// --------------------------------------------------------------------------------------- sums
+template <int TABLE, int VEC>
+__device__ __forceinline__ void write_row(typename RowType<TABLE>::T* row, const Span& at, const f32x8_row& acc, float scale, bool accumulate) {
+  auto* p = row + at.col;
+  f32x8_row y = acc * scale;
+  if constexpr (VEC == 1) {
+    RowType<TABLE>::store1(p, accumulate ? RowType<TABLE>::load1(p) + y[0] : y[0]);
+  } else if (at.skip == 0) {
+    if (accumulate) y += RowType<TABLE>::widen(RowType<TABLE>::load_raw(p));
+    RowType<TABLE>::store(p, y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= at.skip) RowType<TABLE>::store1(p + i, accumulate ? RowType<TABLE>::load1(p + i) + y[i] : y[i]);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void put_part(float* p, const f32x8_row& acc) {
+  if constexpr (VEC == 8) RowType<HBP_F32>::store(p, acc);
+  else *p = acc[0];
+}
+
+struct Sorted {
+  const uint32_t *keys, *order;
+  float* part;  // [chunk][2][dim]: the end of a run that began earlier; the beginning of one that goes on
+  int chunk, n_chunks;
+};
+
+template <int ROW, int TABLE, int VEC, int U>
+__global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, Sorted s, const typename RowType<ROW>::T* d_out,
+                                                                typename RowType<TABLE>::T* d_table, bool accumulate, int log2_tpr) {
+  const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> log2_tpr);
+  const int c = blockIdx.x * (kRowThreads >> log2_tpr) + sub;
+  const int v = (blockIdx.y << log2_tpr) + (threadIdx.x & ((1 << log2_tpr) - 1));
+  const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
+  if (c >= s.n_chunks || v >= n_vec) return;
+  const Span at = span_of<VEC>(v, p.dim);
+  const int first = c * s.chunk, last = min(first + s.chunk, p.T);
+  uint32_t cur = s.keys[first];
+  if (cur >= (uint32_t)p.V) return;  // no tokens from here on
+  bool from_before = first > 0 && s.keys[first - 1] == cur;
+  f32x8_row acc = {};
+  auto end_run = [&](bool goes_on) {
+    if (from_before || goes_on) put_part<VEC>(s.part + ((int64_t)c * 2 + (from_before ? 0 : 1)) * p.dim + at.col, acc);
+    else write_row<TABLE, VEC>(d_table + (int64_t)cur * p.table_st, at, acc, p.scale, accumulate);
+  };
+  for (int i = first; i < last; i += U) {
+    f32x8_row x[U];
+    uint32_t k[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      k[u] = i + u < last ? s.keys[i + u] : (uint32_t)p.V;
+      x[u] = f32x8_row{};
+      if (k[u] < (uint32_t)p.V) x[u] = load_span<ROW, VEC>(d_out + (int64_t)s.order[i + u] * p.row_st + at.col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u >= last) break;
+      if (k[u] != cur) {
+        end_run(false);
+        if (k[u] >= (uint32_t)p.V) return;
+        cur = k[u];
+        from_before = false;
+        acc = f32x8_row{};
+      }
+      acc += x[u];
+    }
+  }
+  end_run(last < p.T && s.keys[last] == cur);
+}
+
+// The run that begins in chunk c and goes beyond it: its parts, in the chunks' order.
+template <int TABLE, int VEC>
+__global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, Sorted s, typename RowType<TABLE>::T* d_table, bool accumulate, int log2_tpr) {
+  const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> log2_tpr);
+  const int c = blockIdx.x * (kRowThreads >> log2_tpr) + sub;
+  if (c + 1 >= s.n_chunks) return;  // nothing goes beyond the last one
+  const int first = c * s.chunk, next = first + s.chunk;
+  const uint32_t k = s.keys[next - 1];
+  if (k >= (uint32_t)p.V || s.keys[next] != k) return;
+  if (s.keys[first] == k && first > 0 && s.keys[first - 1] == k) return;  // it began earlier
+  int n = 0;  // chunks behind this one that begin with the run
+  for (int lane = threadIdx.x & 63;; lane += 64) {
+    const int64_t at = (int64_t)(c + 1 + lane) * s.chunk;
+    const uint64_t in = __builtin_amdgcn_ballot_w64(at < p.T && s.keys[at < p.T ? at : 0] == k);
+    n += __popcll(in);
+    if (~in) break;
+  }
+  const int v = (blockIdx.y << log2_tpr) + (threadIdx.x & ((1 << log2_tpr) - 1));
+  const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
+  if (v >= n_vec) return;
+  const Span at = span_of<VEC>(v, p.dim);
+  const float* part = s.part + (int64_t)c * 2 * p.dim + at.col;
+  f32x8_row acc = load_span<HBP_F32, VEC>(part + p.dim);
+  constexpr int U = 8;
+  for (int i = 1; i <= n; i += U) {
+    f32x8_row x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = i + u <= n ? load_span<HBP_F32, VEC>(part + (int64_t)(i + u) * 2 * p.dim) : f32x8_row{};
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc += x[u];
+  }
+  write_row<TABLE, VEC>(d_table + (int64_t)k * p.table_st, at, acc, p.scale, accumulate);
+}
+
+template <int TABLE, int ROW, int VEC>
+void lookup(const EmbedParams& p, const void* table, void* out, hipStream_t s) {
+  const int log2_tpr = log2_threads_per_row(n_vectors(p.dim)), per_pass = kRowThreads >> log2_tpr;
+  const int64_t passes = ((int64_t)p.T + per_pass - 1) / per_pass;
+  const auto* w = (const typename RowType<TABLE>::T*)table;
+  auto* y = (typename RowType<ROW>::T*)out;
+  if (passes >= 8 * 1024)
+    hipLaunchKernelGGL((embed_lookup_kernel<TABLE, ROW, VEC, 8>), dim3((unsigned)((passes + 7) / 8)), dim3(kRowThreads), 0, s, p, w, y, log2_tpr);
+  else
+    hipLaunchKernelGGL((embed_lookup_kernel<TABLE, ROW, VEC, 1>), dim3((unsigned)passes), dim3(kRowThreads), 0, s, p, w, y, log2_tpr);
+}
+
+template <int ROW, int TABLE, int VEC>
+int sums(const EmbedParams& p, const Sorted& srt, const void* d_out, void* d_table, bool accumulate, hipStream_t s) {
+  const int n_vec = n_vectors(p.dim), log2_tpr = log2_threads_per_row(n_vec), per_group = kRowThreads >> log2_tpr;
+  const dim3 grid((unsigned)((srt.n_chunks + per_group - 1) / per_group), (unsigned)((n_vec + (1 << log2_tpr) - 1) >> log2_tpr));
+  auto* w = (typename RowType<TABLE>::T*)d_table;
+  hipLaunchKernelGGL((embed_sum_kernel<ROW, TABLE, VEC, 8>), grid, dim3(kRowThreads), 0, s, p, srt, (const typename RowType<ROW>::T*)d_out, w, accumulate, log2_tpr);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || srt.n_chunks < 2) return (int)e;
+  hipLaunchKernelGGL((embed_join_kernel<TABLE, VEC>), grid, dim3(kRowThreads), 0, s, p, srt, w, accumulate, log2_tpr);
+  return (int)hipGetLastError();
+}
+
+template <int ROUNDS>
+int sort_one(const EmbedParams& p, int bits, uint32_t* keys, uint32_t* order, const Fill& fill, hipStream_t s) {
+  constexpr int lds = sort_one_lds<ROUNDS>();
+  static bool attr_set = false;
+  if (!attr_set) {
+    const hipError_t e = hipFuncSetAttribute((const void*)embed_sort_one_kernel<ROUNDS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return (int)e;
+    attr_set = true;
+  }
+  hipLaunchKernelGGL((embed_sort_one_kernel<ROUNDS>), dim3(1 + fill.blocks), dim3(kSortThreads), lds, s, p.tokens, p.T, p.V, bits, keys, order, fill);
+  return (int)hipGetLastError();
+}
+
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+int launch_embed_fwd(const EmbedParams& p, int table_type, int row_type, const void* table, void* out, hipStream_t s) {
+  const bool wide = p.dim >= 8;
+  if (table_type == HBP_BF16 && row_type == HBP_BF16) wide ? lookup<HBP_BF16, HBP_BF16, 8>(p, table, out, s) : lookup<HBP_BF16, HBP_BF16, 1>(p, table, out, s);
+  else if (table_type == HBP_BF16) wide ? lookup<HBP_BF16, HBP_F32, 8>(p, table, out, s) : lookup<HBP_BF16, HBP_F32, 1>(p, table, out, s);
+  else if (row_type == HBP_BF16) wide ? lookup<HBP_F32, HBP_BF16, 8>(p, table, out, s) : lookup<HBP_F32, HBP_BF16, 1>(p, table, out, s);
+  else wide ? lookup<HBP_F32, HBP_F32, 8>(p, table, out, s) : lookup<HBP_F32, HBP_F32, 1>(p, table, out, s);
+  return (int)hipGetLastError();
+}
+
+EmbedBwdLayout embed_bwd_layout(int32_t T, int32_t V, int32_t dim) {
+  EmbedBwdLayout l;
+  l.chunk = T <= kSmallChunks ? 16 : 32;
+  l.n_chunks = (T + l.chunk - 1) / l.chunk;
+  const size_t ints = up((size_t)T * 4), tiles = (size_t)(T / kTile + 1);
+  l.keys_off[0] = 0;
+  l.order_off[0] = ints;
+  const bool one = T <= kOneTile;  // sorted where it ends
+  l.keys_off[1] = one ? 0 : 2 * ints;
+  l.order_off[1] = one ? ints : 3 * ints;
+  l.hist_off = one ? 2 * ints : 4 * ints;
+  l.part_off = l.hist_off + (one ? 0 : up(tiles * kDigits * 4));
+  // fewer tokens never need more: a workspace for the longest pack serves all
+  const size_t parts = (size_t)(T <= kSmallChunks ? l.n_chunks : l.n_chunks > kSmallChunks / 16 ? l.n_chunks : kSmallChunks / 16);
+  l.total = l.part_off + up(parts * 2 * (size_t)dim * 4);
+  (void)V;
+  return l;
+}
+
+int launch_embed_bwd(const EmbedParams& p, int table_type, int row_type, const void* d_out, void* d_table, bool accumulate,
+                     char* ws, hipStream_t s) {
+  const EmbedBwdLayout l = embed_bwd_layout(p.T, p.V, p.dim);
+  const int es = table_type == HBP_BF16 ? 2 : 4, bits = key_bits(p.V);
+  uint32_t* keys[2] = {(uint32_t*)(ws + l.keys_off[0]), (uint32_t*)(ws + l.keys_off[1])};
+  uint32_t* order[2] = {(uint32_t*)(ws + l.order_off[0]), (uint32_t*)(ws + l.order_off[1])};
+  Fill fill{(char*)d_table, p.table_st * es, (int64_t)p.dim * es, p.V, 0, 1, 0};
+  // workgroups of 16 wavefronts, a row a wavefront at a time
+  const int fill_blocks = accumulate ? 0 : (int)((p.V + kSortWaves - 1) / kSortWaves < 2048 ? (p.V + kSortWaves - 1) / kSortWaves : 2048);
+  int at = 0;
+  if (p.T <= kOneTile) {
+    fill.blocks = fill_blocks;
+    if (p.T == 0 && accumulate) return 0;
+    const int e = p.T <= 4096 ? sort_one<4>(p, bits, keys[0], order[0], fill, s) : sort_one<16>(p, bits, keys[0], order[0], fill, s);
+    if (e || p.T == 0) return e;
+  } else {
+    const int tiles = (p.T + kTile - 1) / kTile, passes = (bits + kDigitBits - 1) / kDigitBits;
+    uint32_t* hist = (uint32_t*)(ws + l.hist_off);
+    fill.parts = 2 * passes;
+    fill.blocks = (fill_blocks + fill.parts - 1) / fill.parts;
+    for (int pass = 0; pass < passes; ++pass) {
+      const uint32_t* from = pass ? keys[at] : nullptr;
+      const int shift = pass * kDigitBits, to = at ^ 1;
+      fill.part = 2 * pass;
+      hipLaunchKernelGGL(embed_count_kernel, dim3(tiles + fill.blocks), dim3(kSortThreads), 0, s, p.tokens, from, p.T, p.V, shift, tiles, hist, fill);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return (int)e;
+      fill.part = 2 * pass + 1;
+      hipLaunchKernelGGL(embed_scatter_kernel, dim3(tiles + fill.blocks), dim3(kSortThreads), 0, s, p.tokens, from, pass ? order[at] : nullptr,
+                         p.T, p.V, shift, tiles, hist, keys[to], order[to], fill);
+      e = hipGetLastError();
+      if (e != hipSuccess) return (int)e;
+      at = to;
+    }
+  }
+  const Sorted srt{keys[at], order[at], (float*)(ws + l.part_off), l.chunk, l.n_chunks};
+  const bool wide = p.dim >= 8;
+  if (row_type == HBP_BF16 && table_type == HBP_BF16)
+    return wide ? sums<HBP_BF16, HBP_BF16, 8>(p, srt, d_out, d_table, accumulate, s) : sums<HBP_BF16, HBP_BF16, 1>(p, srt, d_out, d_table, accumulate, s);
+  if (row_type == HBP_BF16)
+    return wide ? sums<HBP_BF16, HBP_F32, 8>(p, srt, d_out, d_table, accumulate, s) : sums<HBP_BF16, HBP_F32, 1>(p, srt, d_out, d_table, accumulate, s);
+  if (table_type == HBP_BF16)
+    return wide ? sums<HBP_F32, HBP_BF16, 8>(p, srt, d_out, d_table, accumulate, s) : sums<HBP_F32, HBP_BF16, 1>(p, srt, d_out, d_table, accumulate, s);
+  return wide ? sums<HBP_F32, HBP_F32, 8>(p, srt, d_out, d_table, accumulate, s) : sums<HBP_F32, HBP_F32, 1>(p, srt, d_out, d_table, accumulate, s);
+}
+
+}  // namespace hbp

@@ -135,5 +135,121 @@ class PackedAttention:
         return np.frombuffer(buf.cpu().numpy().tobytes(), dtype=B.PROFILE_DTYPE)
 
 
+_TYPES = {torch.bfloat16: B.HBP_BF16, torch.float32: B.HBP_F32}
+
+
+def _check(name: str, t, device: torch.device, dtype, shape) -> None:
+    """A tensor on the object's device, of the type and shape that it was made for; rows may have a stride."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError("%s: a tensor on %s is wanted" % (name, device))
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: %s %s is wanted, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+
+
+def _device(device) -> torch.device:
+    if not torch.cuda.is_available():
+        raise RuntimeError("a GPU is needed: there is no CPU fallback")
+    B.load_library()
+    d = torch.device(device)
+    return d if d.index is not None else torch.device(d.type, torch.cuda.current_device())
+
+
+class PackedEmbedding:
+    """Token embedding of packs of ``total_tokens`` tokens, and its gradient.  Tokens are int32; one outside
+    [0, vocab) is none: a row of zeros, no gradient.  Calls run on the device's current stream."""
+
+    def __init__(self, total_tokens: int, vocab: int, dim: int, scale: float = 1.0,
+                 table_type: torch.dtype = torch.bfloat16, out_type: torch.dtype = torch.bfloat16,
+                 device: str = "cuda:0"):
+        if table_type not in _TYPES or out_type not in _TYPES:
+            raise ValueError("types: torch.bfloat16 or torch.float32")
+        self.device = _device(device)
+        self.T, self.vocab, self.dim = int(total_tokens), int(vocab), int(dim)
+        self.table_type, self.out_type = table_type, out_type
+        self.desc = B.EmbedDesc(total_tokens=self.T, vocab=self.vocab, dim=self.dim, table_type=_TYPES[table_type],
+                                row_type=_TYPES[out_type], scale=float(scale))
+        self.ws_bytes = B.hbp_embed_bwd_workspace_bytes(self.desc)
+        self.ws = None
+        self.out = torch.zeros((self.T, self.dim), dtype=out_type, device=self.device)
+
+    def _rows(self, name: str, t: torch.Tensor, dtype, n: int) -> int:
+        """Stride of [n, dim] rows in elements; overlapping or scattered rows are refused."""
+        _check(name, t, self.device, dtype, (n, self.dim))
+        if (self.dim > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < self.dim):
+            raise ValueError("%s: rows of adjacent elements are wanted" % name)
+        return t.stride(0) if n > 1 else self.dim
+
+    def _call(self, table: torch.Tensor, rows: torch.Tensor, tokens: torch.Tensor) -> int:
+        _check("tokens", tokens, self.device, torch.int32, (self.T,))
+        if not tokens.is_contiguous():
+            raise ValueError("tokens: a contiguous tensor is wanted")
+        self.desc.table_stride = self._rows("table", table, self.table_type, self.vocab)
+        self.desc.row_stride = self._rows("rows", rows, self.out_type, self.T)
+        return int(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def forward(self, table: torch.Tensor, tokens: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """scale * table[tokens]; into this object's buffer unless ``out`` is given."""
+        out = self.out if out is None else out
+        stream = self._call(table, out, tokens)
+        with torch.cuda.device(self.device):
+            B.hbp_embed_fwd(self.desc, table, tokens, out, stream)
+        return out
+
+    def backward(self, d_out: torch.Tensor, tokens: torch.Tensor, d_table: torch.Tensor,
+                 accumulate: bool = False) -> torch.Tensor:
+        """The table's gradient into ``d_table``, added to what it holds with ``accumulate``."""
+        stream = self._call(d_table, d_out, tokens)
+        if self.ws is None:
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            B.hbp_embed_bwd(self.desc, d_out, tokens, accumulate, d_table, self.ws, stream)
+        return d_table
+
+
+class GradientClip:
+    """The norm of a list of gradients over all their elements, and clipping to it, in place or into ``outs``.  The
+    tensors (contiguous, bf16 or fp32) are held and named by their addresses: make another object when the list
+    changes."""
+
+    def __init__(self, tensors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None,
+                 device: str = "cuda:0"):
+        self.device = _device(device)
+        self.tensors, self.outs = list(tensors), None if outs is None else list(outs)
+        if self.outs is not None and len(self.outs) != len(self.tensors):
+            raise ValueError("outs: one for each tensor")
+        for i, t in enumerate(self.tensors + (self.outs or [])):
+            like = self.tensors[i % max(1, len(self.tensors))]
+            if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype not in _TYPES or not t.is_contiguous():
+                raise ValueError("gradients: contiguous bf16 or fp32 tensors on %s are wanted" % self.device)
+            if t.dtype != like.dtype or t.shape != like.shape:
+                raise ValueError("outs: the tensors' types and shapes are wanted")
+        self.list = B.GradList([t.data_ptr() for t in self.tensors], [t.numel() for t in self.tensors],
+                               [_TYPES[t.dtype] for t in self.tensors],
+                               None if self.outs is None else [t.data_ptr() for t in self.outs])
+        self.sumsq_buf = torch.zeros(1, dtype=torch.float64, device=self.device)
+        self.norm = torch.zeros((), dtype=torch.float32, device=self.device)
+        self.ws = torch.empty(B.hbp_grad_workspace_bytes(self.list.n), dtype=torch.uint8, device=self.device)
+
+    def sumsq(self, accumulate: bool = False) -> torch.Tensor:
+        """Sum of the squares of all elements (fp64, on the device); ranks with different gradients add it up before
+        ``clip_with``."""
+        with torch.cuda.device(self.device):
+            B.hbp_grad_sumsq(self.list, accumulate, self.sumsq_buf, self.ws,
+                             int(torch.cuda.current_stream(self.device).cuda_stream))
+        return self.sumsq_buf
+
+    def clip_with(self, sumsq: torch.Tensor, max_norm: float) -> torch.Tensor:
+        """Clips to ``max_norm``, the sum of squares given; returns the norm (fp32, on the device)."""
+        _check("sumsq", sumsq, self.device, torch.float64, (1,))
+        with torch.cuda.device(self.device):
+            B.hbp_grad_clip(self.list, sumsq, max_norm, self.norm,
+                            int(torch.cuda.current_stream(self.device).cuda_stream))
+        return self.norm
+
+    def clip(self, max_norm: float) -> torch.Tensor:
+        """Norm of this object's tensors, and clipping to it; returns the norm (fp32, on the device)."""
+        return self.clip_with(self.sumsq(), max_norm)
+
+
 def bf16_tensor_to_f32_numpy(t: torch.Tensor) -> np.ndarray:
     return t.detach().float().cpu().numpy()
