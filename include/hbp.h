@@ -404,6 +404,69 @@ hbp_status hbp_packed_ce(const void* logits, int64_t logit_stride_t, int32_t tot
                          int32_t normalizer, float t_ave, void* dlogits_or_null, float* loss_out,
                          float* token_loss_or_null, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- cross attention to packed states of other lengths --------------------------------------------- */
+
+/* Problem description: n_samples pairs of a run of query rows and a run of keys (an encoder's states, an image's patches),
+ * each side packed with bounds of its own, cu_q and cu_kv (int32 [n_samples + 1]).  Either side of a sample may be empty.
+ * Layouts, head dims and strides as in hbp_attn_desc: Q [Tq,Hq,d_qk], K [Tk,Hkv,d_qk], V [Tk,Hkv,d_v], O/dO [Tq,Hq,d_v],
+ * LSE [Hq,Tq] fp32 dense. */
+typedef struct {
+  int32_t total_queries, total_keys, n_samples;
+  int32_t n_q_heads, n_kv_heads;
+  int32_t d_qk, d_v;
+  float softmax_scale; /* <= 0: 1/sqrt(d_qk) */
+  int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h;
+  int64_t v_stride_t, v_stride_h, o_stride_t, o_stride_h;
+} hbp_cross_desc;
+
+/* Rows per tile that the kernels expect from hbp_cross_plan: which = HBP_FWD: query tokens of a query tile (256 divided by the
+ * number of query heads that share a kv head's stream, so it goes by the heads and by Q's and O's strides); HBP_BWD: keys of a
+ * key tile. */
+hbp_status hbp_cross_tile_rows(const hbp_cross_desc* desc, int32_t which, int32_t* rows_out);
+
+/*
+ * hbp_cross_plan — host only.  The bounds of a pack of n_samples pairs of lengths (0 allowed on either side), and its work
+ * list: kind HBP_TILES_QUERY: every sample's query rows in tiles of tile_rows, most keys first; HBP_TILES_KEY: its keys in
+ * tiles, most query rows first (ties by sample, tile).  *pairs_out = sum over samples of query rows times keys.
+ * Size query and capacities as in hbp_pack_plan: cu_q and cu_kv (both or neither; cu_cap each) and tiles may be NULL.
+ * Errors: INVALID_ARG (null pointers, negative lengths or sizes, tile_rows < 1, bad kind, a side of more than INT32_MAX
+ * rows), CAPACITY, NO_MEMORY.
+ */
+hbp_status hbp_cross_plan(const int32_t* q_lengths, const int32_t* kv_lengths, int32_t n_samples, int32_t tile_rows,
+                          int32_t kind, int32_t* cu_q, int32_t* cu_kv, int32_t cu_cap, hbp_tile* tiles, int32_t tile_cap,
+                          int32_t* n_tiles_out, int64_t* pairs_out);
+
+/* Bytes of device workspace a call needs (256-byte aligned base; 0: none): which = HBP_FWD or HBP_BWD. */
+hbp_status hbp_cross_workspace_bytes(const hbp_cross_desc* desc, int32_t which, size_t* bytes_out);
+
+/*
+ * hbp_cross_attn_fwd — O and per-row LSE of attention from every query row of a sample to all keys of the sample.
+ *
+ *   S[r,k] = scale * <Q[r,h,:], K[k,kh,:]>  for cu_q[i] <= r < cu_q[i+1], cu_kv[i] <= k < cu_kv[i+1];  kh = h/(Hq/Hkv)
+ *   LSE[h,r] = ln sum_k exp(S[r,k]);  O[r,h,:] = sum_k exp(S[r,k]-LSE[h,r]) V[k,kh,:]
+ *   a sample without keys: O = 0, LSE = -inf
+ *
+ * Precision as hbp_varlen_attn_fwd (bf16 MFMA, fp32 accumulation and statistics, probabilities rounded to bf16 in front of
+ * the product with V).  q_tiles: the HBP_TILES_QUERY list of hbp_cross_plan made with hbp_cross_tile_rows(..., HBP_FWD).
+ * Malformed tiles are skipped, rows in no tile left untouched.  No tiles: no-op.  All pointers but desc: DEVICE.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, DEVICE, by the rules of hbp_varlen_attn_fwd (k and v may be null where
+ * there are no keys); nothing is launched then.
+ */
+hbp_status hbp_cross_attn_fwd(const hbp_cross_desc* desc, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                              const int32_t* cu_kv, const hbp_tile* q_tiles, int32_t n_q_tiles, void* o, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * hbp_cross_attn_bwd — dQ, dK, dV of L = sum(O * dO) for the attention above; o and lse are the forward's outputs.
+ * Formulas, precision and determinism as hbp_varlen_attn_bwd (no atomics, a repeated call gives the same bits).  dQ of rows of
+ * a sample without keys and dK and dV of keys of a sample without query rows are zeros.  q_tiles as in the forward, kv_tiles:
+ * the HBP_TILES_KEY list made with hbp_cross_tile_rows(..., HBP_BWD); rows and keys in no tile are left untouched.
+ */
+hbp_status hbp_cross_attn_bwd(const hbp_cross_desc* desc, const void* q, const void* k, const void* v, const void* o,
+                              const float* lse, const void* d_o, const int32_t* cu_q, const int32_t* cu_kv,
+                              const hbp_tile* q_tiles, int32_t n_q_tiles, const hbp_tile* kv_tiles, int32_t n_kv_tiles,
+                              void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- token embedding of a packed buffer ------------------------------------------------------------ */
 
 enum { HBP_BF16 = 0, HBP_F32 = 1 }; /* element types */

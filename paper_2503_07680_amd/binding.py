@@ -18,7 +18,8 @@ EXPORTED_SYMBOLS = ["hbp_status_string", "hbp_pack_plan", "hbp_order_query_tiles
                     "hbp_profile_capacity", "hbp_varlen_attn_fwd", "hbp_varlen_attn_bwd", "hbp_varlen_attn_bwd_static",
                     "hbp_set_kernel_events", "hbp_mfma_probe", "hbp_balance_packing",
                     "hbp_packed_ce_workspace_bytes", "hbp_packed_ce", "hbp_auto_select",
-                    "hbp_embed_fwd", "hbp_embed_bwd_workspace_bytes", "hbp_embed_bwd",
+                    "hbp_cross_tile_rows", "hbp_cross_plan", "hbp_cross_workspace_bytes", "hbp_cross_attn_fwd",
+                    "hbp_cross_attn_bwd", "hbp_embed_fwd", "hbp_embed_bwd_workspace_bytes", "hbp_embed_bwd",
                     "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip"]
 
 # numpy views of hbp_pack / hbp_batch
@@ -66,6 +67,17 @@ class AttnDesc(ctypes.Structure):
                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("d_qk", ctypes.c_int32), ("d_v", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float), ("fwd_tile_rows", ctypes.c_int32),
+                ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+                ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+                ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
+                ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64)]
+
+
+class CrossDesc(ctypes.Structure):
+    """Mirror of ``hbp_cross_desc``."""
+    _fields_ = [("total_queries", ctypes.c_int32), ("total_keys", ctypes.c_int32), ("n_samples", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("d_qk", ctypes.c_int32), ("d_v", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
                 ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
                 ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
@@ -135,6 +147,18 @@ def load_library():
     lib.hbp_mfma_probe.argtypes = [i32, i32, vp, vp]
     lib.hbp_auto_select.restype = i32
     lib.hbp_auto_select.argtypes = [vp, i32, vp, i32, i32, i32, ctypes.POINTER(Profile), vp, vp, i32p, i32p]
+    crossp = ctypes.POINTER(CrossDesc)
+    lib.hbp_cross_tile_rows.restype = i32
+    lib.hbp_cross_tile_rows.argtypes = [crossp, i32, i32p]
+    lib.hbp_cross_plan.restype = i32
+    lib.hbp_cross_plan.argtypes = [vp, vp, i32, i32, i32, vp, vp, i32, vp, i32, i32p, i64p]
+    lib.hbp_cross_workspace_bytes.restype = i32
+    lib.hbp_cross_workspace_bytes.argtypes = [crossp, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.hbp_cross_attn_fwd.restype = i32
+    lib.hbp_cross_attn_fwd.argtypes = [crossp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.hbp_cross_attn_bwd.restype = i32
+    lib.hbp_cross_attn_bwd.argtypes = [crossp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp,
+                                       ctypes.c_size_t, vp]
     embedp, sizep = ctypes.POINTER(EmbedDesc), ctypes.POINTER(ctypes.c_size_t)
     lib.hbp_embed_fwd.restype = i32
     lib.hbp_embed_fwd.argtypes = [embedp, vp, vp, vp, vp]
@@ -365,6 +389,64 @@ def hbp_packed_ce(logits, logit_stride_t: int, total_tokens: int, vocab: int, la
                                       _ptr(stream))
     if st != 0:
         raise HbpError(st, "hbp_packed_ce")
+
+
+def hbp_cross_tile_rows(desc: CrossDesc, which: int) -> int:
+    out = ctypes.c_int32()
+    st = load_library().hbp_cross_tile_rows(ctypes.byref(desc), int(which), ctypes.byref(out))
+    if st != 0:
+        raise HbpError(st, "hbp_cross_tile_rows")
+    return int(out.value)
+
+
+def hbp_cross_plan(q_lengths: Sequence[int], kv_lengths: Sequence[int], tile_rows: int, kind: int):
+    """Returns (cu_q int32[n+1], cu_kv int32[n+1], tiles int32[n_tiles,4], pairs).  Host only."""
+    lib = load_library()
+    Q, K = np.ascontiguousarray(q_lengths, dtype=np.int32), np.ascontiguousarray(kv_lengths, dtype=np.int32)
+    if Q.ndim != 1 or Q.shape != K.shape:
+        raise HbpError(1, "hbp_cross_plan")
+    at = lambda a: a.ctypes.data if a.size else None
+    n_tiles, pairs = ctypes.c_int32(), ctypes.c_int64()
+    args = (at(Q), at(K), int(Q.size), int(tile_rows), int(kind))
+    out = (ctypes.byref(n_tiles), ctypes.byref(pairs))
+    st = lib.hbp_cross_plan(*args, None, None, 0, None, 0, *out)
+    if st != 0:
+        raise HbpError(st, "hbp_cross_plan")
+    cu_q, cu_kv = np.zeros(Q.size + 1, dtype=np.int32), np.zeros(Q.size + 1, dtype=np.int32)
+    tiles = np.zeros((n_tiles.value, 4), dtype=np.int32)
+    st = lib.hbp_cross_plan(*args, at(cu_q), at(cu_kv), cu_q.size, at(tiles), len(tiles), *out)
+    if st != 0:
+        raise HbpError(st, "hbp_cross_plan")
+    return cu_q, cu_kv, tiles, int(pairs.value)
+
+
+def hbp_cross_workspace_bytes(desc: CrossDesc, which: int) -> int:
+    out = ctypes.c_size_t()
+    st = load_library().hbp_cross_workspace_bytes(ctypes.byref(desc), int(which), ctypes.byref(out))
+    if st != 0:
+        raise HbpError(st, "hbp_cross_workspace_bytes")
+    return int(out.value)
+
+
+def hbp_cross_attn_fwd(desc: CrossDesc, q, k, v, cu_q, cu_kv, q_tiles, n_q_tiles: int, o, lse, workspace,
+                       stream: Optional[int] = None) -> None:
+    """Enqueue the forward of cross attention on ``stream``."""
+    st = load_library().hbp_cross_attn_fwd(
+        ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_kv), _ptr(q_tiles), int(n_q_tiles),
+        _ptr(o), _ptr(lse), _ptr(workspace), 0 if workspace is None else _nbytes(workspace), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_cross_attn_fwd")
+
+
+def hbp_cross_attn_bwd(desc: CrossDesc, q, k, v, o, lse, d_o, cu_q, cu_kv, q_tiles, n_q_tiles: int, kv_tiles,
+                       n_kv_tiles: int, dq, dk, dv, workspace, stream: Optional[int] = None) -> None:
+    """Enqueue the backward of cross attention on ``stream``."""
+    st = load_library().hbp_cross_attn_bwd(
+        ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(cu_q), _ptr(cu_kv),
+        _ptr(q_tiles), int(n_q_tiles), _ptr(kv_tiles), int(n_kv_tiles), _ptr(dq), _ptr(dk), _ptr(dv),
+        _ptr(workspace), 0 if workspace is None else _nbytes(workspace), stream)
+    if st != 0:
+        raise HbpError(st, "hbp_cross_attn_bwd")
 
 
 HBP_BF16, HBP_F32 = 0, 1

@@ -3,9 +3,12 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <vector>
 
+#include "common.hpp"
+#include "cross_rules.hpp"
 #include "rows.hpp"
 
 namespace {
@@ -84,7 +87,137 @@ bool overlaps(const void* const* in, void* const* out, const int64_t* sizes, con
   return false;
 }
 
+constexpr int64_t kMaxTokenStride = int64_t{1} << 22;  // elements: rows of a tile are addressed in 32 bits, as in hbp_varlen_attn_*
+
+hbp_status check_cross(const hbp_cross_desc* d) {
+  if (!d) return HBP_ERR_INVALID_ARG;
+  if (d->total_queries < 0 || d->total_keys < 0 || d->n_samples < 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->d_qk <= 0 || d->d_v <= 0)
+    return HBP_ERR_INVALID_ARG;
+  if (!std::isfinite(d->softmax_scale)) return HBP_ERR_INVALID_ARG;
+  if (d->n_q_heads % d->n_kv_heads) return HBP_ERR_SHAPE;
+  if (!((d->d_qk == 64 && d->d_v == 64) || (d->d_qk == 128 && d->d_v == 128) || (d->d_qk == 192 && d->d_v == 128))) return HBP_ERR_UNSUPPORTED;
+  const hbp::CrossStrides s = hbp::cross_strides(*d);
+  const int64_t t[4] = {s.q_t, s.k_t, s.v_t, s.o_t}, h[4] = {s.q_h, s.k_h, s.v_h, s.o_h}, dim[4] = {d->d_qk, d->d_qk, d->d_v, d->d_v};
+  for (int i = 0; i < 4; ++i)
+    if (t[i] % 8 || h[i] % 8 || t[i] < dim[i] || h[i] < dim[i] || t[i] > kMaxTokenStride) return HBP_ERR_SHAPE;
+  // the kernels count folded rows, and steps over them, in 32 bits
+  if (((int64_t)d->total_queries << hbp::cross_fold_log2(*d)) > INT32_MAX || (int64_t)d->total_queries * d->n_q_heads > ((int64_t)1 << 36))
+    return HBP_ERR_UNSUPPORTED;
+  return HBP_OK;
+}
+float scale_of(const hbp_cross_desc* d) { return d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / std::sqrt((float)d->d_qk); }
+bool aligned16(const void* p) { return aligned_to(p, 16); }
+constexpr float kLog2e = 1.4426950408889634f;
+
 }  // namespace
+
+extern "C" hbp_status hbp_cross_tile_rows(const hbp_cross_desc* desc, int32_t which, int32_t* rows_out) {
+  if (!rows_out || (which != HBP_FWD && which != HBP_BWD)) return HBP_ERR_INVALID_ARG;
+  const hbp_status st = check_cross(desc);
+  if (st != HBP_OK) return st;
+  *rows_out = which == HBP_BWD ? hbp::kCrossKeys : hbp::kCrossRows >> hbp::cross_fold_log2(*desc);
+  return HBP_OK;
+}
+
+extern "C" hbp_status hbp_cross_workspace_bytes(const hbp_cross_desc* desc, int32_t which, size_t* bytes_out) {
+  if (!bytes_out || (which != HBP_FWD && which != HBP_BWD)) return HBP_ERR_INVALID_ARG;
+  const hbp_status st = check_cross(desc);
+  if (st != HBP_OK) return st;
+  *bytes_out = which == HBP_FWD ? 0 : hbp::cross_bwd_layout(*desc).total;
+  return HBP_OK;
+}
+
+extern "C" hbp_status hbp_cross_attn_fwd(const hbp_cross_desc* desc, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                                         const int32_t* cu_kv, const hbp_tile* q_tiles, int32_t n_q_tiles, void* o, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  const hbp_status st = check_cross(desc);
+  if (st != HBP_OK) return st;
+  if (n_q_tiles < 0) return HBP_ERR_INVALID_ARG;
+  (void)workspace;
+  (void)workspace_bytes;
+  if (desc->total_queries == 0 || n_q_tiles == 0) return HBP_OK;
+  if (!q || !o || !lse || !cu_q || !cu_kv || !q_tiles || (desc->total_keys > 0 && (!k || !v))) return HBP_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return HBP_ERR_INVALID_ARG;
+  const hbp::CrossStrides s = hbp::cross_strides(*desc);
+  hbp::FwdParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.o = static_cast<uint16_t*>(o);
+  p.lse = lse;
+  p.cu = cu_q;
+  p.cu_kv = cu_kv;
+  p.tiles = q_tiles;
+  p.n_tiles = n_q_tiles;
+  p.n_samples = desc->n_samples;
+  p.T = desc->total_queries;
+  p.Tk = desc->total_keys;
+  p.Hq = desc->n_q_heads;
+  p.Hkv = desc->n_kv_heads;
+  p.fold_log2 = hbp::cross_fold_log2(*desc);
+  p.g = (desc->n_q_heads / desc->n_kv_heads) >> p.fold_log2;
+  p.q_st = s.q_t; p.q_sh = s.q_h; p.k_st = s.k_t; p.k_sh = s.k_h;
+  p.v_st = s.v_t; p.v_sh = s.v_h; p.o_st = s.o_t; p.o_sh = s.o_h;
+  p.scale_log2 = scale_of(desc) * kLog2e;
+  return hbp::launch_cross_fwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
+}
+
+extern "C" hbp_status hbp_cross_attn_bwd(const hbp_cross_desc* desc, const void* q, const void* k, const void* v, const void* o,
+                                         const float* lse, const void* d_o, const int32_t* cu_q, const int32_t* cu_kv,
+                                         const hbp_tile* q_tiles, int32_t n_q_tiles, const hbp_tile* kv_tiles, int32_t n_kv_tiles,
+                                         void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream) {
+  const hbp_status st = check_cross(desc);
+  if (st != HBP_OK) return st;
+  if (n_q_tiles < 0 || n_kv_tiles < 0) return HBP_ERR_INVALID_ARG;
+  const hbp::CrossBwdLayout lay = hbp::cross_bwd_layout(*desc);
+  if (lay.total > 0 && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < lay.total)) return HBP_ERR_WORKSPACE;
+  const bool queries = desc->total_queries > 0, keys = desc->total_keys > 0;
+  if (!queries) n_q_tiles = 0;
+  if (!keys) n_kv_tiles = 0;
+  if (n_q_tiles == 0 && n_kv_tiles == 0) return HBP_OK;
+  if (!cu_q || !cu_kv || (n_q_tiles > 0 && !q_tiles) || (n_kv_tiles > 0 && !kv_tiles)) return HBP_ERR_INVALID_ARG;
+  if ((queries && (!q || !o || !lse || !d_o || !dq)) || (keys && (!k || !v || !dk || !dv))) return HBP_ERR_INVALID_ARG;
+  for (const void* x : {q, k, v, o, d_o, (const void*)dq, (const void*)dk, (const void*)dv})
+    if (!aligned16(x)) return HBP_ERR_INVALID_ARG;
+  const hbp::CrossStrides s = hbp::cross_strides(*desc);
+  char* const ws = static_cast<char*>(workspace);
+  hbp::BwdParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.o = static_cast<const uint16_t*>(o);
+  p.d_o = static_cast<const uint16_t*>(d_o);
+  p.lse = lse;
+  p.dq = static_cast<uint16_t*>(dq);
+  p.dk = static_cast<uint16_t*>(dk);
+  p.dv = static_cast<uint16_t*>(dv);
+  p.D = reinterpret_cast<float*>(ws + lay.d_off);
+  p.lse2 = reinterpret_cast<float*>(ws + lay.lse2_off);
+  p.cu = cu_q;
+  p.cu_kv = cu_kv;
+  p.tiles = kv_tiles;
+  p.n_tiles = n_kv_tiles;
+  p.q_tiles = q_tiles;
+  p.n_q_tiles = n_q_tiles;
+  p.n_samples = desc->n_samples;
+  p.T = desc->total_queries;
+  p.Tk = desc->total_keys;
+  p.Hq = desc->n_q_heads;
+  p.Hkv = desc->n_kv_heads;
+  p.fold_log2 = hbp::cross_fold_log2(*desc);
+  p.g = (desc->n_q_heads / desc->n_kv_heads) >> p.fold_log2;
+  p.q_st = s.q_t; p.q_sh = s.q_h; p.k_st = s.k_t; p.k_sh = s.k_h;
+  p.v_st = s.v_t; p.v_sh = s.v_h; p.o_st = s.o_t; p.o_sh = s.o_h;
+  p.scale = scale_of(desc);
+  p.scale_log2 = p.scale * kLog2e;
+  p.n_split = lay.parts;
+  p.n_split_dq = 1;
+  p.dk_part = reinterpret_cast<float*>(ws + lay.dk_part_off);
+  p.dv_part = reinterpret_cast<float*>(ws + lay.dv_part_off);
+  return hbp::launch_cross_bwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
+}
 
 extern "C" hbp_status hbp_embed_fwd(const hbp_embed_desc* desc, const void* table, const int32_t* tokens, void* rows, void* stream) {
   hbp::EmbedParams p;

@@ -33,6 +33,14 @@ __device__ __forceinline__ BwdArgs* bwd_args() {
   return a;
 }
 
+// Part `part` of n_parts of an item's steps.
+struct StepRange {
+  int from, to;
+};
+__device__ __forceinline__ StepRange part_of_steps(int64_t steps, int part, int n_parts) {
+  return {__builtin_amdgcn_readfirstlane((int)(steps * part / n_parts)), __builtin_amdgcn_readfirstlane((int)(steps * (part + 1) / n_parts))};
+}
+
 struct ProfAcc {
   uint32_t n_done = 0;
   uint64_t t_first = 0, t_last = 0, t_busy = 0, t0 = 0;
@@ -100,8 +108,12 @@ struct DqLds {
   }
 };
 
-template <int DQK, int DV, int HALVES = 1, bool SHARED = false, bool DIRECT = HALVES == 2>
+//
+// CROSS: cross attention.  An item is 128 folded rows (see Fold) of a query tile for one folded group of heads; every row sees
+// all keys of its sample.
+template <int DQK, int DV, int HALVES = 1, bool SHARED = false, bool DIRECT = HALVES == 2, bool CROSS = false>
 __device__ __forceinline__ void dq_items(int block) {
+  static_assert(!CROSS || (DIRECT && HALVES == 1), "heads are folded into rows");
   using Lds = DqLds<DQK, DV, HALVES, SHARED>;
   constexpr int BM = 128, BN = 64;
   constexpr int KRB = DQK * 2, VRB = DV * 2;
@@ -163,7 +175,10 @@ __device__ __forceinline__ void dq_items(int block) {
     const BwdArgs& p = *bwd_args<!DIRECT>();
     const WorkQueues wq{p.counter_dq, p.n_q_tiles, p.Hkv * p.n_split_dq, quotient(p.g / (SHARED ? 2 : 1), p.n_split_dq)};
     int tile_idx, h;
-    if constexpr (!DIRECT) {
+    if constexpr (CROSS) {
+      tile_idx = blockIdx.z;
+      h = blockIdx.x;
+    } else if constexpr (!DIRECT) {
       if (!next_item(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, h)) break;
     } else {
       const Taken tk = SHARED || HALVES == 1 ? direct_item_inline(wq.n_tiles, wq.Hkv, wq.per_kv, 0, 0, block)
@@ -176,12 +191,23 @@ __device__ __forceinline__ void dq_items(int block) {
     hbp_tile tl;
     int s0, s1;
     bool ok = load_tile(p.q_tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
-    if (ok) {
+    int ks0 = 0, ks1 = 0;
+    if constexpr (CROSS) {
+      if (ok) {
+        ks0 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample]);
+        ks1 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample + 1]);
+        ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+             tl.row_end - tl.row_begin <= 2 * BM >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
+             BM * (int)blockIdx.y < (tl.row_end - tl.row_begin) << p.fold_log2;
+      }
+    } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
            tl.row_end <= s1 && tl.row_end - tl.row_begin <= BM;
     }
     if (ok) {
-      const int r0 = tl.row_begin, r1 = tl.row_end;
+      // CROSS: rows of the tile, folded, from 0 on
+      const int r0 = CROSS ? BM * (int)blockIdx.y : tl.row_begin;
+      const int r1 = CROSS ? min(r0 + BM, (tl.row_end - tl.row_begin) << p.fold_log2) : tl.row_end;
       const bool has_head = HALVES == 1 || SHARED || h < p.Hq;  // an odd number of heads: the last pair has one
       if (!has_head) h = p.Hq - 1;
       if (HALVES == 2) h = __builtin_amdgcn_readfirstlane(h);
@@ -190,10 +216,10 @@ __device__ __forceinline__ void dq_items(int block) {
       const int my_row = r0 + 32 * wave + l32;
       const bool row_valid = has_head && my_row < r1;
       const bool wave_active = has_head && r0 + 32 * wave < r1;
-      const int n_keys = r1 - s0;
+      const int n_keys = CROSS ? ks1 - ks0 : r1 - s0, first_key = CROSS ? ks0 : s0;
       const int nkt = (n_keys + BN - 1) / BN;
-      const uint16_t* kbase = p.k + (int64_t)s0 * p.k_st + (int64_t)kh * p.k_sh;
-      const uint16_t* vbase = p.v + (int64_t)s0 * p.v_st + (int64_t)kh * p.v_sh;
+      const uint16_t* kbase = p.k + (int64_t)first_key * p.k_st + (int64_t)kh * p.k_sh;
+      const uint16_t* vbase = p.v + (int64_t)first_key * p.v_st + (int64_t)kh * p.v_sh;
 
       // copy `slot` of this wave's share of key tile kt (K first, then V)
       constexpr int NKCP = decltype(k_loader)::PER_WAVE, NVCP = decltype(v_loader)::PER_WAVE;
@@ -215,12 +241,32 @@ __device__ __forceinline__ void dq_items(int block) {
       Frag qf[NC], dof[NCV];
       float lse2 = INFINITY, Dv = 0.f;  // +inf: rows past the tile end get probability 0
       if (row_valid) {
-        lse2 = p.lse2[(int64_t)h * p.T + my_row];
-        Dv = p.D[(int64_t)h * p.T + my_row];
+        const int64_t at = CROSS ? (((int64_t)h * p.T + tl.row_begin) << p.fold_log2) + my_row : (int64_t)h * p.T + my_row;
+        lse2 = p.lse2[at];
+        Dv = p.D[at];
       }
       const uint32_t lds_all = lds_address(smem_all);
       const int first_row = r0 + 32 * wave;  // of this wave
-      {
+      if constexpr (CROSS) {
+        const int64_t token = tl.row_begin + (first_row >> p.fold_log2);
+        const uint16_t* q_rows = p.q + token * p.q_st + (int64_t)(h << p.fold_log2) * p.q_sh;
+        const uint16_t* do_rows = p.d_o + token * p.o_st + (int64_t)(h << p.fold_log2) * p.o_sh;
+        const Fold q_fold{p.fold_log2, (uint32_t)p.q_st * 2, (uint32_t)p.q_sh * 2}, o_fold{p.fold_log2, (uint32_t)p.o_st * 2, (uint32_t)p.o_sh * 2};
+        const uint32_t q_at = Lds::q_at(lds_all, wave_in_wg), do_at = Lds::do_at(lds_all, wave_in_wg);
+        const int rows = r1 - first_row;
+        RowStage<DQK>::copy_in(q_rows, q_fold, rows, q_at, lane);
+        if (Lds::kBoth) RowStage<DV>::copy_in(do_rows, o_fold, rows, do_at, lane);
+        if (nkt > 0) issue(0);
+        wait_async_but<NKCP + NVCP>();
+        RowStage<DQK>::fragments(q_at, lane, qf);
+        if constexpr (!Lds::kBoth) {
+          wait_lds_reads();
+          RowStage<DV>::copy_in(do_rows, o_fold, rows, do_at, lane);
+          wait_async_loads();
+        }
+        RowStage<DV>::fragments(do_at, lane, dof);
+        race_fence();
+      } else {
         const uint16_t* q_rows = p.q + (int64_t)first_row * p.q_st + (int64_t)h * p.q_sh;
         const uint16_t* do_rows = p.d_o + (int64_t)first_row * p.o_st + (int64_t)h * p.o_sh;
         const uint32_t q_at = Lds::q_at(lds_all, wave_in_wg), do_at = Lds::do_at(lds_all, wave_in_wg);
@@ -249,7 +295,7 @@ __device__ __forceinline__ void dq_items(int block) {
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dqacc[db][i] = 0.f;
-      const int q_in = qw0 + l32;
+      const int q_in = CROSS ? n_keys - 1 : qw0 + l32;  // the last key that this lane's query sees
 
       // One 32-key block: sd = (S^T, dP^T - D) products, sm = dS^T = exp2(c S^T - LSE2)(dP^T - D),
       // gr = dQ^T += K^T dS^T.  Interior tiles pipeline their two blocks inside the wave:
@@ -342,7 +388,7 @@ __device__ __forceinline__ void dq_items(int block) {
         if (point && (kt & 1) != cur_buf) point_offsets_at(kt & 1);
       };
 
-      const int n_interior = wave_active ? min(nkt, (qw0 + 1) / BN) : 0;
+      const int n_interior = !wave_active ? 0 : CROSS ? n_keys / BN : min(nkt, (qw0 + 1) / BN);
       // One interior tile.  BUF = kt & 1 as a compile-time constant: the lane's offsets stay on buffer 0
       // and the reads carry the buffer in their immediate offsets; BUF < 0: the offsets follow the buffers.
       auto interior_tile = [&](auto bufc, int kt) {
@@ -352,7 +398,9 @@ __device__ __forceinline__ void dq_items(int block) {
         Blk x0, x1;
         LdsChain<NC + NCV, PD> c1;
         c1.prefill(sd_load(0, BUF));
-        c1.template run_with<NKCP + NVCP>(sd_load(0, BUF), sd_mma(x0), [&](int slot) { issue_slot(kt + 1, slot); });
+        c1.template run_with<NKCP + NVCP>(sd_load(0, BUF), sd_mma(x0), [&](int slot) {
+          if (!CROSS || kt + 1 < nkt) issue_slot(kt + 1, slot);
+        });
         c1.prefill(sd_load(1, BUF));
         if (kVgprScores) mfma_results_ready(x0.s, x0.dp);
         c1.template run_with<17>(sd_load(1, BUF), sd_mma(x1), [&](int k) { sm_slice(x0, k_off, k, std::false_type{}); });
@@ -394,11 +442,11 @@ __device__ __forceinline__ void dq_items(int block) {
       for (; kt < nkt; ++kt) {  // tiles that touch the diagonal: plain masked path, block by block
         begin_tile(kt);
         const int k_off = kt * BN;
-        if (!wave_active || k_off > qw0 + 31) continue;
+        if (!wave_active || (!CROSS && k_off > qw0 + 31)) continue;
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
           const int kb = k_off + 32 * blk;
-          if (kb > qw0 + 31) continue;
+          if (CROSS ? kb >= n_keys : kb > qw0 + 31) continue;
           Blk x;
           LdsChain<NC + NCV, PD> c1;
           c1.prefill(sd_load(blk));
@@ -415,11 +463,17 @@ __device__ __forceinline__ void dq_items(int block) {
       }
       if (cur_buf) point_offsets_at(0);
 
+      if (CROSS && nkt == 0) wait_async_loads();  // no tile has waited for the rows
       __syncthreads();  // the tiles are no longer read
       race_fence();
       if (wave_active) {
         const uint32_t at = lds_all + wave_in_wg * Lds::UNIT;
         RowStage<DQK>::put(at, lane, dqacc, p.scale);
+        if constexpr (CROSS) {
+          RowStage<DQK>::copy_out(p.dq + (int64_t)(tl.row_begin + (first_row >> p.fold_log2)) * p.q_st + (int64_t)(h << p.fold_log2) * p.q_sh,
+                                  Fold{p.fold_log2, (uint32_t)p.q_st * 2, (uint32_t)p.q_sh * 2}, r1 - first_row, at, lane);
+          break;
+        }
         RowStage<DQK>::copy_out(p.dq + (int64_t)first_row * p.q_st + (int64_t)h * p.q_sh, (uint32_t)p.q_st * 2, r1 - first_row, at, lane);
       }
     }
@@ -450,7 +504,10 @@ struct DkdvLds {
 };
 
 // DIRECT: the launch's item `block` and no other (see bwd_both4_kernel).  n_resident: workgroups under way at a time.
-template <int DQK, int DV, bool DIRECT = false>
+//
+// CROSS: cross attention.  The rows of an item are all folded rows (see Fold) of its sample's queries, in blocks of 64, for each of
+// the g folded groups of heads; n_split > 1: a part of an item is a range of these steps.  No key is masked for any row.
+template <int DQK, int DV, bool DIRECT = false, bool CROSS = false>
 __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
   constexpr int BN = 128, BQ = 64;
   constexpr int QRB = DQK * 2, ORB = DV * 2;
@@ -500,8 +557,16 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
   const uint32_t q_stride_b = (uint32_t)bwd_args<false>()->q_st * 2, o_stride_b = (uint32_t)bwd_args<false>()->o_st * 2;
   FullTileLoader<DQK, BQ> q_loader;
   FullTileLoader<DV, BQ> o_loader;
-  q_loader.init(wave, lane, q_stride_b);
-  o_loader.init(wave, lane, o_stride_b);
+  Fold q_fold{0, q_stride_b, 0}, o_fold{0, o_stride_b, 0};
+  if constexpr (CROSS) {
+    q_fold = Fold{bwd_args<false>()->fold_log2, q_stride_b, (uint32_t)bwd_args<false>()->q_sh * 2};
+    o_fold = Fold{bwd_args<false>()->fold_log2, o_stride_b, (uint32_t)bwd_args<false>()->o_sh * 2};
+    q_loader.init(wave, lane, q_fold);
+    o_loader.init(wave, lane, o_fold);
+  } else {
+    q_loader.init(wave, lane, q_stride_b);
+    o_loader.init(wave, lane, o_stride_b);
+  }
 
   // Both tile buffers start out as zeros: an idle step (see the step loop) multiplies whatever the
   // second buffer holds by zero operands, and that must not be the NaN patterns of unwritten LDS.
@@ -518,9 +583,12 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
   for (;;) {
     const BwdArgs& p = *bwd_args<!DIRECT>();
     const WorkQueues wq{p.counter, p.n_tiles, p.Hkv * p.n_split, 1};
-    const int g_item = quotient(p.g, p.n_split);
+    const int g_item = CROSS ? p.g : quotient(p.g, p.n_split);
     int tile_idx, vh;
-    if constexpr (DIRECT) {
+    if constexpr (CROSS) {
+      tile_idx = blockIdx.z;
+      vh = blockIdx.x;
+    } else if constexpr (DIRECT) {
       const Taken tk = direct_item_inline(wq.n_tiles, wq.Hkv, 1, 0, 0, block);
       tile_idx = __builtin_amdgcn_readfirstlane(tk.tile_idx);
       vh = __builtin_amdgcn_readfirstlane(tk.head);
@@ -528,18 +596,26 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
       if (!next_item(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, vh)) break;
     }
     const int kh = quotient(vh, p.n_split), part = vh - kh * p.n_split;
-    const int head0 = vh * g_item;  // first query head of the item
+    const int head0 = CROSS ? (kh * g_item) << p.fold_log2 : vh * g_item;  // first query head of the item
     prof_begin(pa, profiled, tid);
 
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
-    if (ok) {
+    bool ok = load_tile(p.tiles, tile_idx, CROSS ? p.cu_kv : p.cu, p.n_samples, lane, tl, s0, s1);
+    int qs0 = 0, qs1 = 0;
+    if constexpr (CROSS) {
+      if (ok) {
+        qs0 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample]);
+        qs1 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample + 1]);
+        ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+             tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
+      }
+    } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
            tl.row_end <= s1 && tl.row_end - tl.row_begin <= BN;
     }
     if (ok) {
-      const int s_len = s1 - s0;
+      const int s_len = CROSS ? (qs1 - qs0) << p.fold_log2 : s1 - s0;  // rows
       const int k0_in = tl.row_begin - s0;
       const int kw0_in = k0_in + 32 * wave;
       const int my_key = tl.row_begin + 32 * wave + l32;
@@ -547,9 +623,10 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
       const bool wave_active = tl.row_begin + 32 * wave < tl.row_end;
       const int key_in = kw0_in + l32;
 
-      const int qb_start = (k0_in / BQ) * BQ;
+      const int qb_start = CROSS ? 0 : (k0_in / BQ) * BQ;
       const int nqb = (s_len - qb_start + BQ - 1) / BQ;
-      const int n_steps = nqb * g_item;
+      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, p.n_split) : StepRange{0, nqb * g_item};
+      const int n_steps = range.to - range.from;
 
       // Step order: the query blocks from the LAST one of the sample down to the tile's own, and for each
       // block the g query heads of the group.  Every key tile of a sample needs a suffix of the same
@@ -566,20 +643,22 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
       // (With fewer than 8 workgroups per kv head there is little to share and the plain order is kept.)
       const int w_share = quotient(n_resident, min(p.Hkv * p.n_split, kNumXcd * kHeadGroup));  // heads in work at a time
       const int set = quotient(tl.tile, max(w_share, 1));
-      int skip = w_share >= 8 && (set & 1) ? (tl.tile - set * w_share) * (BN / BQ) : 0;
+      int skip = !CROSS && w_share >= 8 && (set & 1) ? (tl.tile - set * w_share) * (BN / BQ) : 0;
       skip = max(0, min(skip, nqb - 1));
+      if (CROSS) skip = range.from / g_item;
       const int first_blk = nqb - 1 - skip;
       // the blocks are taken in the order first_blk .. 0, then nqb-1 .. first_blk+1, g steps each
       // Copies are issued in step order; the source pointers of the next block to copy are carried
       // along instead of being recomputed from the step number.
-      const int64_t first_row = (int64_t)s0 + qb_start + (int64_t)first_blk * BQ;
+      const int fold = CROSS ? p.fold_log2 : 0;
+      const int64_t first_row = CROSS ? (int64_t)qs0 + ((first_blk * BQ) >> fold) : (int64_t)s0 + qb_start + (int64_t)first_blk * BQ;
       const uint16_t* q_blk = p.q + first_row * p.q_st + (int64_t)head0 * p.q_sh;
       const uint16_t* o_blk = p.d_o + first_row * p.o_st + (int64_t)head0 * p.o_sh;
-      const float* row_blk = (wave == 0 ? p.lse2 : p.D) + (int64_t)head0 * p.T + first_row;
-      const uint16_t* q_src = q_blk;
-      const uint16_t* o_src = o_blk;
-      const float* row_src = row_blk;
-      int blk_next = first_blk, head_next = 0;
+      const float* row_blk = (wave == 0 ? p.lse2 : p.D) + ((int64_t)(head0 >> fold) * p.T << fold) + (first_row << fold);
+      int blk_next = first_blk, head_next = CROSS ? range.from - skip * g_item : 0;
+      const uint16_t* q_src = q_blk + (int64_t)(head_next << fold) * p.q_sh;
+      const uint16_t* o_src = o_blk + (int64_t)(head_next << fold) * p.o_sh;
+      const float* row_src = row_blk + ((int64_t)head_next * p.T << fold);
       // The copies of a step's operands are issued one at a time (slot 0 .. N_COPY-1), so that they can sit
       // behind the MFMAs of the step before; taking the last slot moves the source on to the next step.
       // qb_in[buf]: first query row (in-sample) of the block whose copies went to buffer buf.
@@ -592,9 +671,11 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
         const int valid = FULL ? BQ : s_len - qb_start - blk_next * BQ;  // >= 1; < BQ only for the sample's last block
         if (slot < NQC) {
           if (FULL) q_loader.issue_full(slot, q_src, q_lds + buf * Q_TILE, wave);
+          else if (CROSS) q_loader.issue_one(slot, q_src, q_fold, valid, q_lds + buf * Q_TILE, wave, lane);
           else q_loader.issue_one(slot, q_src, q_stride_b, valid, q_lds + buf * Q_TILE, wave, lane);
         } else if (slot < NQC + NOC) {
           if (FULL) o_loader.issue_full(slot - NQC, o_src, o_lds + buf * O_TILE, wave);
+          else if (CROSS) o_loader.issue_one(slot - NQC, o_src, o_fold, valid, o_lds + buf * O_TILE, wave, lane);
           else o_loader.issue_one(slot - NQC, o_src, o_stride_b, valid, o_lds + buf * O_TILE, wave, lane);
         } else {
           if (wave < 2) {
@@ -609,16 +690,16 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
             head_next = 0;
             const int64_t jump = blk_next == 0 ? (int64_t)(nqb - 1) * BQ : -(int64_t)BQ;
             blk_next = blk_next == 0 ? nqb - 1 : blk_next - 1;
-            q_blk += jump * p.q_st;
-            o_blk += jump * p.o_st;
+            q_blk += (jump >> fold) * p.q_st;  // whole tokens
+            o_blk += (jump >> fold) * p.o_st;
             row_blk += jump;
             q_src = q_blk;
             o_src = o_blk;
             row_src = row_blk;
           } else {
-            q_src += p.q_sh;
-            o_src += p.o_sh;
-            row_src += p.T;
+            q_src += p.q_sh << fold;
+            o_src += p.o_sh << fold;
+            row_src += (int64_t)p.T << fold;
           }
         }
       };
@@ -757,7 +838,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
           float pr = e_val;
           if (decltype(masked)::value) {
             const int q_in = qb + 32 * sub + 8 * b + 4 * hh + v;
-            if (key_in > q_in || q_in >= s_len) pr = 0.f;
+            if ((!CROSS && key_in > q_in) || q_in >= s_len) pr = 0.f;
           }
           const float ds = pr * x.dp[i];
           if (i & 1) {
@@ -797,10 +878,10 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
         c1.prefill(sd_load(0));
         init_dp(xa, 0);  // behind the operand reads: only the first dP MFMA needs it
         // not in reach: the block lies above this wave's keys, or this is the idle step that makes the count even
-        const bool in_reach = wave_active && active && qb + BQ - 1 >= kw0_in;
-        const bool need_a = in_reach && qb + 31 >= kw0_in;           // qb < s_len always holds
-        const bool need_b = in_reach && qb + 63 >= kw0_in && qb + 32 < s_len;
-        const bool any_mask = kw0_in + 31 > qb || qb + 63 >= s_len;  // diagonal or sample tail in reach
+        const bool in_reach = wave_active && active && (CROSS || qb + BQ - 1 >= kw0_in);
+        const bool need_a = in_reach && (CROSS || qb + 31 >= kw0_in);  // qb < s_len always holds
+        const bool need_b = in_reach && (CROSS || qb + 63 >= kw0_in) && qb + 32 < s_len;
+        const bool any_mask = (!CROSS && kw0_in + 31 > qb) || qb + 63 >= s_len;  // diagonal or sample tail in reach
         const bool pair = need_a && need_b && !any_mask;
         if (pair) {
           // a next block with all its rows (every block but a sample's last) is copied slot by slot behind
@@ -844,7 +925,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int q_in = qb + 32 + 8 * (i >> 2) + 4 * hh + (i & 3);
-              if (key_in > q_in || q_in >= s_len) xb.s[i] = -INFINITY;
+              if ((!CROSS && key_in > q_in) || q_in >= s_len) xb.s[i] = -INFINITY;
             }
           } else {
 #pragma unroll
@@ -879,6 +960,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
         race_fence();
       }
 
+      if (CROSS && n_steps == 0) wait_async_loads();  // no query rows: no step has waited for the rows of K and V
       if (p.n_split == 1) {
         if (wave_active) {  // both through the wave's rows of K
           RowStage<DQK>::put(k_at, lane, dkt, -p.scale);
@@ -888,7 +970,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
         }
       } else if (key_valid) {
         // this part's sums, fp32, [part][key][kv head][dim]; the reduce kernel adds the parts up
-        const int64_t row = ((int64_t)part * p.T + my_key) * p.Hkv + kh;
+        const int64_t row = ((int64_t)part * (CROSS ? p.Tk : p.T) + my_key) * p.Hkv + kh;
         float* dkp = p.dk_part + row * DQK + 4 * hh;
         float* dvp = p.dv_part + row * DV + 4 * hh;
         const float ksc = -p.scale;
@@ -950,7 +1032,10 @@ __global__ __launch_bounds__(kThreads, 1) void bwd_both4_kernel(const BwdParams,
 // groups half a step apart (+2 %); s_setprio around the MFMA chains; copies with a wait of their own in mid-step.
 //
 // DIRECT: the launch's item `block` and no other (see bwd_both_kernel).  n_resident: workgroups under way at a time.
-template <int DQK, int DV, bool DIRECT = false>
+//
+// CROSS: cross attention, as in dkdv_items.  What is copied from behind the sample's rows is zeros (Q, dO, LSE2 and D): their
+// probability is 1 and multiplies zeros, so nothing is masked at all.
+template <int DQK, int DV, bool DIRECT = false, bool CROSS = false>
 __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
   static_assert(DQK == DV, "one set of lane offsets for Q and dO");
   constexpr int BN = 128, BQ = 64, SUB = 32, NBUF = 3;
@@ -996,8 +1081,16 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
 
   const uint32_t q_stride_b = (uint32_t)bwd_args<false>()->q_st * 2, o_stride_b = (uint32_t)bwd_args<false>()->o_st * 2;
   FullTileLoader<DQK, SUB> q_loader, o_loader;
-  q_loader.init(kg, lane, q_stride_b);
-  o_loader.init(kg, lane, o_stride_b);
+  Fold q_fold{0, q_stride_b, 0}, o_fold{0, o_stride_b, 0};
+  if constexpr (CROSS) {
+    q_fold = Fold{bwd_args<false>()->fold_log2, q_stride_b, (uint32_t)bwd_args<false>()->q_sh * 2};
+    o_fold = Fold{bwd_args<false>()->fold_log2, o_stride_b, (uint32_t)bwd_args<false>()->o_sh * 2};
+    q_loader.init(kg, lane, q_fold);
+    o_loader.init(kg, lane, o_fold);
+  } else {
+    q_loader.init(kg, lane, q_stride_b);
+    o_loader.init(kg, lane, o_stride_b);
+  }
 
   const bool profiled = !DIRECT && bwd_args<false>()->prof;
   ProfAcc pa;
@@ -1005,9 +1098,12 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
   for (;;) {
     const BwdArgs& p = *bwd_args<!DIRECT>();
     const WorkQueues wq{p.counter, p.n_tiles, p.Hkv * p.n_split, 1};
-    const int g_item = quotient(p.g, p.n_split);
+    const int g_item = CROSS ? p.g : quotient(p.g, p.n_split);
     int tile_idx, vh;
-    if constexpr (DIRECT) {
+    if constexpr (CROSS) {
+      tile_idx = blockIdx.z;
+      vh = blockIdx.x;
+    } else if constexpr (DIRECT) {
       const Taken tk = direct_item_inline(wq.n_tiles, wq.Hkv, 1, 0, 0, block);
       tile_idx = __builtin_amdgcn_readfirstlane(tk.tile_idx);
       vh = __builtin_amdgcn_readfirstlane(tk.head);
@@ -1015,49 +1111,61 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
       if (!next_item(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, vh)) break;
     }
     const int kh = quotient(vh, p.n_split), part = vh - kh * p.n_split;
-    const int head0 = vh * g_item;
+    const int head0 = CROSS ? (kh * g_item) << p.fold_log2 : vh * g_item;
     prof_begin(pa, profiled, wave);
 
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
-    if (ok) {
+    bool ok = load_tile(p.tiles, tile_idx, CROSS ? p.cu_kv : p.cu, p.n_samples, lane, tl, s0, s1);
+    int qs0 = 0, qs1 = 0;
+    if constexpr (CROSS) {
+      if (ok) {
+        qs0 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample]);
+        qs1 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample + 1]);
+        ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+             tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
+      }
+    } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
            tl.row_end <= s1 && tl.row_end - tl.row_begin <= BN;
     }
     if (ok) {
-      const int s_len = s1 - s0;
+      const int fold = CROSS ? p.fold_log2 : 0;
+      const int s_len = CROSS ? (qs1 - qs0) << fold : s1 - s0;  // rows
       const int k0_in = tl.row_begin - s0;
       const int kw0_in = k0_in + 32 * kg;
       const int my_key = tl.row_begin + 32 * kg + l32;
       const bool key_valid = my_key < tl.row_end;
       const bool wave_active = tl.row_begin + 32 * kg < tl.row_end;
 
-      const int qb_start = (k0_in / BQ) * BQ;
+      const int qb_start = CROSS ? 0 : (k0_in / BQ) * BQ;
       const int nqb = (s_len - qb_start + BQ - 1) / BQ;
-      const int n_steps = nqb * g_item;
+      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, p.n_split) : StepRange{0, nqb * g_item};
+      const int n_steps = range.to - range.from;
       const int w_share = quotient(n_resident, min(p.Hkv * p.n_split, kNumXcd * kHeadGroup));
       const int set = quotient(tl.tile, max(w_share, 1));
-      int skip = w_share >= 8 && (set & 1) ? (tl.tile - set * w_share) * (BN / BQ) : 0;
+      int skip = !CROSS && w_share >= 8 && (set & 1) ? (tl.tile - set * w_share) * (BN / BQ) : 0;
       skip = max(0, min(skip, nqb - 1));
+      if (CROSS) skip = range.from / g_item;
       // Step order as in the four-wave kernel.  The copies of a step's operands run two steps ahead, one by one behind the
       // updates: their address path takes 16 clocks of the compute unit a copy, and a burst of them holds the waves.  State of the copying side: the block and head of the next
       // step to copy, its first row of this group's 32 (in-sample), the steps left, and the descriptors of the three
       // sources (Q, dO, and LSE2 or D: waves 0 and 1 of a group copy those).
-      int blk_next = nqb - 1 - skip, head_next = 0, copies_left = n_steps;
+      int blk_next = nqb - 1 - skip, head_next = CROSS ? range.from - skip * g_item : 0, copies_left = n_steps;
       int q0_next = qb_start + blk_next * BQ + SUB * qs;
       u32x4 q_desc, o_desc, r_desc;
       auto set_spans = [&]() {
         const int rows = copies_left > 0 ? s_len - q0_next : 0;
-        q_desc[2] = rows_span(rows, SUB, q_stride_b, QRB);
-        o_desc[2] = rows_span(rows, SUB, o_stride_b, QRB);
+        q_desc[2] = CROSS ? q_fold.span(rows, SUB, QRB) : rows_span(rows, SUB, q_stride_b, QRB);
+        o_desc[2] = CROSS ? o_fold.span(rows, SUB, QRB) : rows_span(rows, SUB, o_stride_b, QRB);
         r_desc[2] = kg < 2 ? rows_span(rows, SUB, 4, 4) : 0;
       };
       {
-        const int64_t row = (int64_t)s0 + q0_next;
-        q_desc = buffer_desc(p.q + row * p.q_st + (int64_t)head0 * p.q_sh, 0);
-        o_desc = buffer_desc(p.d_o + row * p.o_st + (int64_t)head0 * p.o_sh, 0);
-        r_desc = buffer_desc((kg == 0 ? p.lse2 : p.D) + (int64_t)head0 * p.T + row, 0);
+        const int64_t row = CROSS ? (int64_t)qs0 + (q0_next >> fold) : (int64_t)s0 + q0_next;
+        const int head = head0 + (CROSS ? head_next << fold : 0);
+        q_desc = buffer_desc(p.q + row * p.q_st + (int64_t)head * p.q_sh, 0);
+        o_desc = buffer_desc(p.d_o + row * p.o_st + (int64_t)head * p.o_sh, 0);
+        r_desc = buffer_desc((kg == 0 ? p.lse2 : p.D) + ((int64_t)(head >> fold) * p.T << fold) + (row << fold), 0);
         set_spans();
       }
       constexpr int NQC = decltype(q_loader)::PER_WAVE, N_COPY = 2 * NQC + 1;
@@ -1069,16 +1177,16 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
         else buffer_copy4<BUF * 1024>(r_desc, lane * 4, rows_lds);
       };
       // to the first head of the block before, from the last head of a block
-      const int64_t q_blk = -2 * ((int64_t)BQ * p.q_st + (int64_t)(g_item - 1) * p.q_sh);
-      const int64_t o_blk = -2 * ((int64_t)BQ * p.o_st + (int64_t)(g_item - 1) * p.o_sh);
-      const int64_t r_blk = -4 * ((int64_t)BQ + (int64_t)(g_item - 1) * p.T);
+      const int64_t q_blk = -2 * ((int64_t)(BQ >> fold) * p.q_st + ((int64_t)(g_item - 1) * p.q_sh << fold));
+      const int64_t o_blk = -2 * ((int64_t)(BQ >> fold) * p.o_st + ((int64_t)(g_item - 1) * p.o_sh << fold));
+      const int64_t r_blk = -4 * ((int64_t)BQ + ((int64_t)(g_item - 1) * p.T << fold));
       auto advance = [&](int buf) {
         q0_in[buf] = q0_next;
         --copies_left;
         if (++head_next < g_item) {
-          buffer_advance(q_desc, 2 * p.q_sh);
-          buffer_advance(o_desc, 2 * p.o_sh);
-          buffer_advance(r_desc, 4 * (int64_t)p.T);
+          buffer_advance(q_desc, 2 * p.q_sh << fold);
+          buffer_advance(o_desc, 2 * p.o_sh << fold);
+          buffer_advance(r_desc, 4 * (int64_t)p.T << fold);
         } else {
           head_next = 0;
           buffer_advance(q_desc, q_blk);
@@ -1088,8 +1196,8 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
           if (--blk_next < 0) {  // on from the tile's own block to the sample's last
             blk_next += nqb;
             q0_next += nqb * BQ;
-            buffer_advance(q_desc, 2 * (int64_t)nqb * BQ * p.q_st);
-            buffer_advance(o_desc, 2 * (int64_t)nqb * BQ * p.o_st);
+            buffer_advance(q_desc, 2 * ((int64_t)nqb * BQ >> fold) * p.q_st);
+            buffer_advance(o_desc, 2 * ((int64_t)nqb * BQ >> fold) * p.o_st);
             buffer_advance(r_desc, 4 * (int64_t)nqb * BQ);
           }
           // only the sample's last block may have fewer rows; and none are copied behind the item's last step
@@ -1152,7 +1260,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
         __builtin_amdgcn_s_waitcnt(0x0F70 + N_COPY);  // all copies but the last step's, which are the next step's operands
         __syncthreads();
         const int q0 = q0_in[BUF];
-        const bool need = ((q0 + 31 - kw0) | (s_len - 1 - q0)) >= 0;  // not above this wave's keys, nor behind the sample
+        const bool need = CROSS ? wave_active && q0 < s_len : ((q0 + 31 - kw0) | (s_len - 1 - q0)) >= 0;  // not above this wave's keys, nor behind the sample
         typedef const __attribute__((address_space(3))) u32x4* lds_u4;
         typedef const __attribute__((address_space(3))) f32x4* lds_f4;
         auto q_load = [&](int i) { Frag a; a.u = *(lds_u4)(uintptr_t)(qoff[i] + BUF * PAIR); return a; };
@@ -1200,7 +1308,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
           mfma32_vgpr(dp, rq[NC % kPD].v, vnat[0].v);
           rq[NC % kPD] = o_load(kPD);
           mfma_result_ready(s);
-          if (((q0 - kw0_in - 31) | (s_len - 32 - q0)) < 0) {  // the diagonal or the sample's end in reach
+          if (!CROSS && ((q0 - kw0_in - 31) | (s_len - 32 - q0)) < 0) {  // the diagonal or the sample's end in reach
             int x = lane;  // opaque: rebuilt here, not held across the loop
             asm volatile("" : "+v"(x));
             const int e0 = q0 + 4 * (x >> 5);
@@ -1313,7 +1421,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
             RowStage<DQK>::copy_out(out + (int64_t)first_key * st + (int64_t)kh * sh, (uint32_t)st * 2, keys_left, at, lane);
           }
         } else if (key_valid) {
-          float* row = parts + (((int64_t)part * p.T + my_key) * p.Hkv + kh) * DQK + 4 * hh;
+          float* row = parts + (((int64_t)part * (CROSS ? p.Tk : p.T) + my_key) * p.Hkv + kh) * DQK + 4 * hh;
 #pragma unroll
           for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -1422,7 +1530,8 @@ size_t bwd_partial_floats(int T, int Hkv, int g, int dim) {
 // kPreSmall pairs 64 a workgroup, or too few loads are under way: 2048 tokens, 32 heads: 7.96 -> 6.88 (256 pairs: 8.12).
 constexpr int64_t kPreSmall = 131072;
 inline int prepass_heads_log2(int Hq) { return Hq >= 8 ? 3 : Hq >= 4 ? 2 : Hq >= 2 ? 1 : 0; }
-template <int DV, int PAIRS>
+// FOLDED (cross attention): D and LSE2 go out as [folded group][token][F].
+template <int DV, int PAIRS, bool FOLDED = false>
 __global__ __launch_bounds__(kThreads) void bwd_prepass_kernel(const BwdParams p, int heads_log2) {
   constexpr int LPR = DV / 8, PER_PASS = kThreads / LPR, PASSES = PAIRS / PER_PASS, BATCH = PASSES < 8 ? PASSES : 8;
   constexpr int PAIRS_LOG2 = __builtin_ctz(PAIRS);
@@ -1471,8 +1580,9 @@ __global__ __launch_bounds__(kThreads) void bwd_prepass_kernel(const BwdParams p
   const int h = h0 + (tid >> rows_log2);
   const int64_t r = r0 + (tid & (rows - 1));
   if (h < p.Hq && r < p.T) {
-    p.D[(int64_t)h * p.T + r] = s[0];
-    p.lse2[(int64_t)h * p.T + r] = p.lse[(int64_t)h * p.T + r] * kLog2e;
+    const int64_t at = FOLDED ? (((int64_t)(h >> p.fold_log2) * p.T + r) << p.fold_log2) + (h & ((1 << p.fold_log2) - 1)) : (int64_t)h * p.T + r;
+    p.D[at] = s[0];
+    p.lse2[at] = p.lse[(int64_t)h * p.T + r] * kLog2e;
   }
 }
 
@@ -1603,6 +1713,82 @@ int launch_bwd(int d_qk, int d_v, const BwdParams& p, int grid_dq, int grid_dkdv
   if (d_qk == 128 && d_v == 128) return launch_bwd_t<128, 128>(p, grid_dq, grid_dkdv, s, ev);
   if (d_qk == 192 && d_v == 128) return launch_bwd_t<192, 128>(p, grid_dq, grid_dkdv, s, ev);
   return (int)hipErrorInvalidValue;
+}
+
+// ------------------------------------------------------------------------------------- cross attention
+// Grids: folded groups of heads (kv heads times parts), halves of a query tile, tiles.
+template <int DQK, int DV>
+__global__ __launch_bounds__(kThreads, DQK <= 128 ? 2 : 1) void cross_dq_kernel(const BwdParams) {
+  dq_items<DQK, DV, 1, false, true, true>(0);
+}
+template <int DQK, int DV>
+__global__ __launch_bounds__(2 * kThreads, 2) void cross_dkdv_eight_kernel(const BwdParams) {
+  dkdv8_items<DQK, DV, true, true>(0, 1);
+}
+template <int DQK, int DV>
+__global__ __launch_bounds__(kThreads, 1) void cross_dkdv_four_kernel(const BwdParams) {
+  dkdv_items<DQK, DV, true, true>(0, 1);
+}
+
+constexpr int kCrossMostTiles = 65535;  // of one launch: the grid's third dimension
+
+template <int DQK, int DV>
+static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
+  constexpr int lds_dq = DqLds<DQK, DV, 1, false>::BYTES;
+  constexpr bool kEight = DQK == DV;
+  constexpr int lds_dkdv = kEight ? dkdv8_lds<DQK, DV>() : DkdvLds<DQK, DV>::bytes();
+  void (*dkdv)(const BwdParams);
+  if constexpr (kEight) dkdv = cross_dkdv_eight_kernel<DQK, DV>;
+  else dkdv = cross_dkdv_four_kernel<DQK, DV>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    hipError_t e = hipFuncSetAttribute((const void*)cross_dq_kernel<DQK, DV>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_dq);
+    if (e != hipSuccess) return (int)e;
+    e = hipFuncSetAttribute((const void*)dkdv, hipFuncAttributeMaxDynamicSharedMemorySize, lds_dkdv);
+    if (e != hipSuccess) return (int)e;
+    attr_set = true;
+  }
+  hipError_t e = hipSuccess;
+  if (p.T > 0) {
+    const bool small = (int64_t)p.T * p.Hq <= kPreSmall;
+    const int hl = prepass_heads_log2(p.Hq), rows = (small ? 64 : 256) >> hl;
+    const dim3 grid((unsigned)(((int64_t)p.T + rows - 1) / rows * ((p.Hq + (1 << hl) - 1) >> hl)));
+    if (small) hipLaunchKernelGGL((bwd_prepass_kernel<DV, 64, true>), grid, dim3(kThreads), 0, s, p, hl);
+    else hipLaunchKernelGGL((bwd_prepass_kernel<DV, 256, true>), grid, dim3(kThreads), 0, s, p, hl);
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  for (int at = 0; at < p.n_tiles; at += kCrossMostTiles) {
+    BwdParams part = p;
+    part.tiles += at;
+    part.n_tiles = p.n_tiles - at < kCrossMostTiles ? p.n_tiles - at : kCrossMostTiles;
+    hipLaunchKernelGGL(dkdv, dim3((unsigned)(p.Hkv * p.n_split), 1, (unsigned)part.n_tiles), dim3(kEight ? 2 * kThreads : kThreads), lds_dkdv, s, part);
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  if (p.n_split > 1) {
+    BwdParams keys = p;  // the reduce kernel's rows are the keys
+    keys.T = p.Tk;
+    keys.cu = p.cu_kv;
+    const int units = 128 * p.Hkv * ((DQK + DV) / 4), share = kThreads * kReduceUnits;
+    hipLaunchKernelGGL((bwd_reduce_parts_kernel<DQK, DV>), dim3(p.n_tiles, (units + share - 1) / share), dim3(kThreads), 0, s, keys);
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  for (int at = 0; at < p.n_q_tiles; at += kCrossMostTiles) {
+    BwdParams part = p;
+    part.q_tiles += at;
+    part.n_q_tiles = p.n_q_tiles - at < kCrossMostTiles ? p.n_q_tiles - at : kCrossMostTiles;
+    hipLaunchKernelGGL((cross_dq_kernel<DQK, DV>), dim3((unsigned)(p.Hkv * p.g), 2, (unsigned)part.n_q_tiles), dim3(kThreads), lds_dq, s, part);
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  return 0;
+}
+int launch_cross_bwd(int d_qk, int d_v, const BwdParams& p, hipStream_t s) {
+  if (d_qk == 64) return launch_cross_bwd_t<64, 64>(p, s);
+  if (d_qk == 128) return launch_cross_bwd_t<128, 128>(p, s);
+  return launch_cross_bwd_t<192, 128>(p, s);
 }
 
 }  // namespace hbp

@@ -226,6 +226,24 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }
 
+// Cross attention has no diagonal, so the F = 2^log2 query heads that read one kv head can be rows beside each other: row r
+// of a run of tokens is head r % F of token r / F, a tile holds 1/F of the tokens, and K and V go through LDS once for all of
+// them.  F is the largest power of two up to 32 in the group size (of the layouts in which a token's heads lie inside its
+// stride, so that a run of whole tokens is one span of memory).
+struct Fold {
+  int log2;
+  uint32_t token, head;  // strides in bytes
+  __device__ __forceinline__ uint32_t offset(int row) const {
+    return (uint32_t)(row >> log2) * token + (uint32_t)(row & ((1 << log2) - 1)) * head;
+  }
+  // bytes that `rows` rows (whole tokens) of row_bytes each span, at most max_rows of them (0 for none)
+  __device__ __forceinline__ uint32_t span(int rows, int max_rows, uint32_t row_bytes) const {
+    if (rows <= 0) return 0;
+    rows = min(rows, max_rows);
+    return (uint32_t)((rows >> log2) - 1) * token + (uint32_t)((1 << log2) - 1) * head + row_bytes;
+  }
+};
+
 // Tile copy with the lane-dependent part (LDS row, swizzled chunk) packed once per kernel.  Rows
 // >= rows_valid re-read the last valid row (never out of bounds; the caller masks their products).
 template <int D, int ROWS, int NW = 4>
@@ -281,6 +299,14 @@ struct FullTileLoader {
       off[ii] = (uint32_t)row * stride_bytes + (uint32_t)(swz<D>(cpos, row) * 16);
     }
   }
+  __device__ __forceinline__ void init(int wave, int lane, const Fold& f) {
+#pragma unroll
+    for (int ii = 0; ii < PER_WAVE; ++ii) {
+      const int pos = (wave + NW * ii) * 1024 + lane * 16;
+      const int row = pos / RB, cpos = (pos % RB) / 16;
+      off[ii] = f.offset(row) + (uint32_t)(swz<D>(cpos, row) * 16);
+    }
+  }
   // copy ii of this wave, every row of the tile valid
   __device__ __forceinline__ void issue_full(int ii, const uint16_t* g, const char* lds_tile, int wave) const {
     if (!has(ii, wave)) return;
@@ -301,6 +327,16 @@ struct FullTileLoader {
                                             const char* lds_tile, int wave, int lane) const {
     if (rows_valid >= ROWS) issue_full(ii, g, lds_tile, wave);
     else issue_clamped(ii, g, stride_bytes, rows_valid, lds_tile, wave, lane);
+  }
+  // folded rows
+  __device__ __forceinline__ void issue_one(int ii, const uint16_t* g, const Fold& f, int rows_valid, const char* lds_tile,
+                                            int wave, int lane) const {
+    if (rows_valid >= ROWS) return issue_full(ii, g, lds_tile, wave);
+    if (!has(ii, wave)) return;
+    asm volatile("" : "+v"(lane));
+    const int pos = (wave + NW * ii) * 1024 + lane * 16;
+    const int row = pos / RB, cpos = (pos % RB) / 16, last = rows_valid - 1;
+    async_copy16(g, f.offset(row < last ? row : last) + (uint32_t)(swz<D>(cpos, row) * 16), lds_address(lds_tile) + (wave + NW * ii) * 1024);
   }
   __device__ __forceinline__ void issue(const uint16_t* g, uint32_t stride_bytes, int rows_valid,
                                         const char* lds_tile, int wave, int lane) const {
@@ -411,13 +447,31 @@ struct RowStage {
     const uint32_t to = lds + (PARTS == 1 ? 0 : part * MINE * 1024);
     copies<0, MINE>(d, at, to);
   }
-  template <int I, int TO>
-  static __device__ __forceinline__ void copies(const u32x4& d, const Places& at, uint32_t to) {
+  template <int I, int TO, class At>
+  static __device__ __forceinline__ void copies(const u32x4& d, const At& at, uint32_t to) {
     if constexpr (I < TO) {
       buffer_copy16<I * 1024>(d, at(I), to);
       copies<I + 1, TO>(d, at, to);
     }
   }
+  // The same for folded rows (see Fold): row r of the wavefront is head r % F of token r / F.
+  static __device__ __forceinline__ void copy_in(const uint16_t* g, const Fold& f, int rows_valid, uint32_t lds, int lane) {
+    race_fence_of_wave();
+    u32x4 d = buffer_desc(g, f.span(rows_valid, 32, RB));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) d[i] = __builtin_amdgcn_readfirstlane(d[i]);
+    asm volatile("s_nop 4" : "+s"(d));
+    const FoldedPlaces at{f, fresh(lane)};
+    copies<0, N>(d, at, lds);
+  }
+  struct FoldedPlaces {
+    const Fold& f;
+    int lane;
+    __device__ __forceinline__ uint32_t operator()(int i) const {
+      const int pos = i * 1024 + lane * 16, r = pos / RB;
+      return f.offset(r) + (uint32_t)(swz<D>((pos % RB) / 16, r) * 16);
+    }
+  };
   // 16-byte chunk 2 * pair + lane / 32 of row lane % 32
   static __device__ __forceinline__ uint32_t at(uint32_t lds, int pair, int lane) {
     return lds + (lane & 31) * RB + swz<D>(2 * pair + (lane >> 5), lane & 31) * 16;
@@ -450,6 +504,19 @@ struct RowStage {
     const auto dst = __builtin_amdgcn_make_buffer_rsrc((void*)((uintptr_t)hi << 32 | lo), 0,
                                                        __builtin_amdgcn_readfirstlane((int)rows_span(rows_valid, 32, stride_bytes, RB)), 0x00020000u);
     const Places place(lane, stride_bytes);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(lds + i * 1024 + lane * 16);
+      __builtin_amdgcn_raw_buffer_store_b128(x, dst, place(i), 0, 0);
+    }
+  }
+  static __device__ __forceinline__ void copy_out(uint16_t* g, const Fold& f, int rows_valid, uint32_t lds, int lane) {
+    race_fence_of_wave();
+    lane = fresh(lane);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)g), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)g >> 32));
+    const auto dst = __builtin_amdgcn_make_buffer_rsrc((void*)((uintptr_t)hi << 32 | lo), 0,
+                                                       __builtin_amdgcn_readfirstlane((int)f.span(rows_valid, 32, RB)), 0x00020000u);
+    const FoldedPlaces place{f, lane};
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const u32x4 x = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(lds + i * 1024 + lane * 16);
@@ -699,6 +766,10 @@ struct FwdParams {
   hbp_profile_rec* prof;
   int32_t n_split;   // the query heads of a kv head are dealt to the dies in this many parts (see heads_split)
   int32_t halves;    // 1: n_tiles counts halves of 256-row tiles
+  // Cross attention alone: bounds of the samples' keys, their number, and the fold of the query heads (see Fold).  g is then
+  // the number of folded groups that read one kv head, and a "head" of an item is such a group.
+  const int32_t* cu_kv;
+  int32_t Tk, fold_log2;
 };
 
 struct BwdParams {
@@ -721,6 +792,10 @@ struct BwdParams {
   // added up in part order by a reduce kernel.
   int32_t n_split, n_split_dq;
   float *dk_part, *dv_part;
+  // Cross attention alone, as in FwdParams; D and lse2 are then [folded group][token][F], and n_split parts of an item's
+  // steps over the query rows (see cross_dkdv).
+  const int32_t* cu_kv;
+  int32_t Tk, fold_log2;
 };
 
 struct CeParams {  // packed cross-entropy
@@ -745,6 +820,8 @@ constexpr int kCeMaxWorkgroups = 2048;
 int launch_fwd(int d_qk, int d_v, const FwdParams& p, int tile_rows, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 // ev: {dkdv start, dkdv stop, dq start, dq stop}, entries may be null
 int launch_bwd(int d_qk, int d_v, const BwdParams& p, int grid_dq, int grid_dkdv, hipStream_t s, hipEvent_t* ev);
+int launch_cross_fwd(int d_qk, int d_v, const FwdParams& p, hipStream_t s);
+int launch_cross_bwd(int d_qk, int d_v, const BwdParams& p, hipStream_t s);
 size_t bwd_partial_floats(int T, int Hkv, int g, int dim);  // per tensor; 0 when the dK/dV kernel needs no partial sums
 // n_cu: compute units to fill (the kernel picks its own workgroup shape and grid)
 int launch_packed_ce(const CeParams& p, int n_cu, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);

@@ -316,9 +316,14 @@ __device__ __forceinline__ FwdArgs* fwd_args() {
 // DIRECT: the workgroup takes one item, by its place in the grid (kv heads, query heads of one, tiles): no function to find
 // it, no divisions and no barriers in front of it (.9 of an item's 20 us at 8192 tokens, 32/8 heads of 128), and without a loop
 // over items 30 registers less: at head size 64 three workgroups of four wavefronts fit a compute unit.
-template <int DQK, int DV, int HP, int TP, bool DIRECT>
+//
+// CROSS: cross attention (see hbp_cross_attn_fwd).  A tile's rows are the folded rows of its tokens (see Fold), TP * 128 of
+// them a workgroup; every row sees all keys of its sample, so all wavefronts have the same blocks and the last one is masked
+// where the keys end.  Always DIRECT.
+template <int DQK, int DV, int HP, int TP, bool DIRECT, bool CROSS = false>
 __device__ __forceinline__ void fwd_items() {
   static_assert(HP * TP <= 2, "eight wavefronts per compute unit");
+  static_assert(!CROSS || (DIRECT && HP == 1), "heads are folded into rows");
   constexpr int NW = 4 * HP * TP;
   using Lds = FwdLds<DQK, DV, NW>;
   using W = FwdWave<DQK, DV>;
@@ -390,7 +395,16 @@ __device__ __forceinline__ void fwd_items() {
     hbp_tile tl;
     int s0, s1;
     bool ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.n_samples, lane, tl, s0, s1);
-    if (ok) {
+    int ks0 = 0, ks1 = 0;
+    if constexpr (CROSS) {
+      if (ok) {
+        ks0 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample]);
+        ks1 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample + 1]);
+        ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+             tl.row_end - tl.row_begin <= (BM << halves) >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
+             BM * half < (tl.row_end - tl.row_begin) << p.fold_log2;
+      }
+    } else if (ok) {
       // tiles start a multiple of 32 rows into their sample: each wave then has exactly one key
       // block that crosses its diagonal
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
@@ -398,18 +412,23 @@ __device__ __forceinline__ void fwd_items() {
            tl.row_begin + BM * half < tl.row_end;
     }
     if (ok) {
-      const int r0 = tl.row_begin + BM * half, r1 = halves ? min(r0 + BM, tl.row_end) : tl.row_end;
+      // CROSS: rows of the tile, folded, from 0 on
+      const int r0 = CROSS ? BM * half : tl.row_begin + BM * half;
+      const int r1 = CROSS ? (halves ? min(r0 + BM, (tl.row_end - tl.row_begin) << p.fold_log2) : (tl.row_end - tl.row_begin) << p.fold_log2)
+                           : halves ? min(r0 + BM, tl.row_end) : tl.row_end;
       const int kh = h / p.g;
       const int qw0 = r0 - s0 + 32 * rw;  // in-sample index of this wave's first query
       const int my_row = r0 + 32 * rw + l32;
       const bool row_valid = my_row < r1;
       const bool wave_active = r0 + 32 * rw < r1;
-      const int nb = wave_active ? qw0 / 32 + 1 : 0;  // this wave's key blocks are 0..nb-1
+      const int n_keys = CROSS ? ks1 - ks0 : r1 - s0;  // keys 0..n_keys-1 (in-sample) are needed by this tile
+      // this wave's key blocks are 0..nb-1
+      const int nb = !wave_active ? 0 : CROSS ? (n_keys + 31) / 32 : qw0 / 32 + 1;
 
-      const int n_keys = r1 - s0;  // keys 0..n_keys-1 (in-sample) are needed by this tile
+      const int first_key = CROSS ? ks0 : s0;
       const int nkt = (n_keys + BN - 1) / BN;  // nb <= 2 nkt
-      const uint16_t* kbase = p.k + (int64_t)s0 * p.k_st + (int64_t)kh * p.k_sh;
-      const uint16_t* vbase = p.v + (int64_t)s0 * p.v_st + (int64_t)kh * p.v_sh;
+      const uint16_t* kbase = p.k + (int64_t)first_key * p.k_st + (int64_t)kh * p.k_sh;
+      const uint16_t* vbase = p.v + (int64_t)first_key * p.v_st + (int64_t)kh * p.v_sh;
       auto issue_k = [&](int t) {
         if (t < nkt)
           k_loader.issue(kbase + (int64_t)t * BN * p.k_st, k_stride_b, n_keys - t * BN, k_lds + (t & 1) * K_TILE, wave, lane);
@@ -421,7 +440,12 @@ __device__ __forceinline__ void fwd_items() {
       // Q fragments (B operand of S^T = K Q^T): lane holds query l32, dims 16c+8hh..+7
       const uint32_t stage = Lds::stage(lds0, wave);
       int rows_left = r1 - (r0 + 32 * rw);
-      if (Lds::kStaged)
+      if constexpr (CROSS) {
+        static_assert(!CROSS || Lds::kStaged, "a folded row is read in whole rows");
+        const int f0 = r0 + 32 * rw;  // its token and head among the folded ones
+        RowStage<DQK>::copy_in(p.q + (int64_t)(tl.row_begin + (f0 >> p.fold_log2)) * p.q_st + (int64_t)(h << p.fold_log2) * p.q_sh,
+                               Fold{p.fold_log2, (uint32_t)p.q_st * 2, (uint32_t)p.q_sh * 2}, rows_left, stage, lane);
+      } else if (Lds::kStaged)
         RowStage<DQK>::copy_in(p.q + (int64_t)(r0 + 32 * rw) * p.q_st + (int64_t)h * p.q_sh, (uint32_t)p.q_st * 2, rows_left, stage, lane);
       asm volatile("" : "+v"(rows_left));  // over the loops in a vector register: scalar ones are short there
       issue_k(0);
@@ -444,7 +468,7 @@ __device__ __forceinline__ void fwd_items() {
         for (int i = 0; i < 16; ++i) w.oacc[eb][i] = 0.f;
       w.m_run = 0.f;
       w.l_run = 0.f;
-      w.q_in = qw0 + l32;
+      w.q_in = CROSS ? n_keys - 1 : qw0 + l32;  // the last key that this lane's query sees
       w.p_cur = w.p_even = w.psum = 0.f;
 
       int k_buf = 0, v_buf = 0;  // buffers the LDS offsets currently point at
@@ -489,7 +513,8 @@ __device__ __forceinline__ void fwd_items() {
 
       // Tiles whose two phases both run every part unmasked (phases 1 .. nb-3) get a loop of
       // their own with one code variant; every wave passes nkt barriers in total.
-      const int t_hot_end = nb >= 6 ? (nb - 4) / 2 + 1 : 1;  // hot tiles are 1 .. t_hot_end-1
+      int t_hot_end = nb >= 6 ? (nb - 4) / 2 + 1 : 1;  // hot tiles are 1 .. t_hot_end-1
+      if (CROSS && nkt == 0) t_hot_end = 0;  // no keys: no tile 0 either
       int t = 0;
       if (nkt > 0) {
         w.template any_phase<0>(0, nb);
@@ -575,8 +600,26 @@ __device__ __forceinline__ void fwd_items() {
       const float l_tot = w.l_run + xor32(w.l_run);
       {
         const FwdArgs& p = *fwd_args<!DIRECT>();
-        const float inv = 1.f / l_tot;
+        const float inv = CROSS && n_keys == 0 ? 0.f : 1.f / l_tot;  // no keys: O = 0, LSE = -inf
         const bool row_valid = l32 < rows_left;
+        if constexpr (CROSS) {
+          const int f0 = r0 + 32 * rw, f = f0 + l32;
+          const int64_t token = tl.row_begin + (f0 >> p.fold_log2);
+          uint16_t* const rows = p.o + token * p.o_st + (int64_t)(h << p.fold_log2) * p.o_sh;
+          const Fold fold{p.fold_log2, (uint32_t)p.o_st * 2, (uint32_t)p.o_sh * 2};
+          if constexpr (Lds::kOwn) {
+            RowStage<DV>::put(stage, lane, w.oacc, inv);
+            RowStage<DV>::copy_out(rows, fold, rows_left, stage, lane);
+          } else {
+            uint16_t* op = rows + fold.offset(l32) / 2;
+#pragma unroll
+            for (int eb = 0; eb < NEB; ++eb) store_block_bf16(op + 32 * eb, w.oacc[eb], inv, hh, row_valid);
+          }
+          if (row_valid && hh == 0)
+            p.lse[(int64_t)((h << p.fold_log2) + (f & ((1 << p.fold_log2) - 1))) * p.T + tl.row_begin + (f >> p.fold_log2)] =
+                n_keys == 0 ? -INFINITY : (w.m_run + log2f(l_tot)) * 0.6931471805599453f;
+          break;
+        }
         if constexpr (Lds::kOwn) {
           RowStage<DV>::put(stage, lane, w.oacc, inv);
           RowStage<DV>::copy_out(p.o + (int64_t)__builtin_amdgcn_readfirstlane(my_row) * p.o_st + (int64_t)h * p.o_sh, (uint32_t)p.o_st * 2,
@@ -618,6 +661,11 @@ __global__ __launch_bounds__(kThreads * HP * TP, 2 / (HP * TP)) void fwd_kernel(
 template <int DQK, int DV, int HP, int TP>
 __global__ __launch_bounds__(kThreads * HP * TP, 2 / (HP * TP)) void fwd_direct_kernel(const FwdParams) {
   fwd_items<DQK, DV, HP, TP, true>();
+}
+
+template <int DQK, int DV, int TP>
+__global__ __launch_bounds__(kThreads * TP, 2 / TP) void cross_forward_kernel(const FwdParams) {
+  fwd_items<DQK, DV, 1, TP, true, true>();
 }
 
 __global__ void zero_counters_kernel(int32_t* c) {
@@ -679,6 +727,44 @@ int launch_fwd(int d_qk, int d_v, const FwdParams& p, int tile_rows, hipStream_t
   if (d_qk == 128 && d_v == 128) return launch_fwd_t<128, 128>(p, tile_rows, s, ev0, ev1);
   if (d_qk == 192 && d_v == 128) return launch_fwd_t<192, 128>(p, tile_rows, s, ev0, ev1);
   return (int)hipErrorInvalidValue;
+}
+
+// ------------------------------------------------------------------------------------- cross attention
+template <int DQK, int DV, int TP>
+static int launch_cross_fwd_t(FwdParams p, hipStream_t s) {
+  constexpr int lds_bytes = FwdLds<DQK, DV, 4 * TP>::bytes();
+  static bool attr_set = false;
+  if (!attr_set) {
+    const hipError_t e = hipFuncSetAttribute((const void*)cross_forward_kernel<DQK, DV, TP>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+    if (e != hipSuccess) return (int)e;
+    attr_set = true;
+  }
+  p.halves = TP == 1;
+  p.n_split = 1;
+  constexpr int kMost = 32767;  // the tiles, or halves of them, are the grid's third dimension
+  for (int at = 0; at < p.n_tiles; at += kMost) {
+    FwdParams part = p;
+    part.tiles += at;
+    part.n_tiles = (p.n_tiles - at < kMost ? p.n_tiles - at : kMost) << p.halves;
+    hipLaunchKernelGGL((cross_forward_kernel<DQK, DV, TP>), dim3((unsigned)(p.Hkv * p.g), 1, (unsigned)part.n_tiles), dim3(kThreads * TP), lds_bytes, s, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  return 0;
+}
+template <int DQK, int DV>
+static int launch_cross_fwd_d(const FwdParams& p, hipStream_t s) {
+  // a 256-row tile a workgroup of eight wavefronts, or, where those would not fill the chip, half of one
+  const bool halves = FwdLds<DQK, DV, 4>::kStaged && (int64_t)p.n_tiles * p.Hkv * p.g <= 2 * kNumCU;
+  if constexpr (FwdLds<DQK, DV, 4>::kStaged) {
+    if (halves) return launch_cross_fwd_t<DQK, DV, 1>(p, s);
+  }
+  return launch_cross_fwd_t<DQK, DV, 2>(p, s);
+}
+int launch_cross_fwd(int d_qk, int d_v, const FwdParams& p, hipStream_t s) {
+  if (d_qk == 64) return launch_cross_fwd_d<64, 64>(p, s);
+  if (d_qk == 128) return launch_cross_fwd_d<128, 128>(p, s);
+  return launch_cross_fwd_d<192, 128>(p, s);
 }
 
 }  // namespace hbp

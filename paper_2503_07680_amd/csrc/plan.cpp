@@ -147,3 +147,68 @@ extern "C" hbp_status hbp_pack_plan(const int32_t* lengths, int32_t n_lengths, i
     return HBP_ERR_INVALID_ARG;
   }
 }
+
+static hbp_status hbp_cross_plan_impl(const int32_t* q_lengths, const int32_t* kv_lengths, int32_t n, int32_t tile_rows, int32_t kind,
+                                      int32_t* cu_q, int32_t* cu_kv, int32_t cu_cap, hbp_tile* tiles, int32_t tile_cap,
+                                      int32_t* n_tiles_out, int64_t* pairs_out) {
+  if (!n_tiles_out || !pairs_out) return HBP_ERR_INVALID_ARG;
+  *n_tiles_out = 0;
+  *pairs_out = 0;
+  if (n < 0 || (n > 0 && (!q_lengths || !kv_lengths)) || tile_rows < 1 || cu_cap < 0 || tile_cap < 0) return HBP_ERR_INVALID_ARG;
+  if ((kind != HBP_TILES_QUERY && kind != HBP_TILES_KEY) || (cu_q == nullptr) != (cu_kv == nullptr)) return HBP_ERR_INVALID_ARG;
+  const bool queries = kind == HBP_TILES_QUERY;
+  int64_t at_q = 0, at_kv = 0, pairs = 0, n_tiles = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (q_lengths[i] < 0 || kv_lengths[i] < 0) return HBP_ERR_INVALID_ARG;
+    at_q += q_lengths[i];
+    at_kv += kv_lengths[i];
+    pairs += (int64_t)q_lengths[i] * kv_lengths[i];
+    n_tiles += ((int64_t)(queries ? q_lengths[i] : kv_lengths[i]) + tile_rows - 1) / tile_rows;
+  }
+  if (at_q > INT32_MAX || at_kv > INT32_MAX) return HBP_ERR_INVALID_ARG;
+  std::vector<Item> items;
+  items.reserve((size_t)n_tiles);
+  int64_t at = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t rows = queries ? q_lengths[i] : kv_lengths[i];
+    int32_t t = 0;
+    for (int64_t lo = 0; lo < rows; lo += tile_rows, ++t) {
+      const int64_t hi = std::min<int64_t>(lo + tile_rows, rows);
+      items.push_back({queries ? kv_lengths[i] : q_lengths[i], {i, t, (int32_t)(at + lo), (int32_t)(at + hi)}});
+    }
+    at += rows;
+  }
+  std::stable_sort(items.begin(), items.end(), [](const Item& a, const Item& b) { return a.cost > b.cost; });
+  *n_tiles_out = (int32_t)items.size();
+  *pairs_out = pairs;
+  hbp_status st = HBP_OK;
+  if (cu_q) {
+    if (cu_cap < n + 1) {
+      st = HBP_ERR_CAPACITY;
+    } else {
+      cu_q[0] = cu_kv[0] = 0;
+      for (int32_t i = 0; i < n; ++i) {
+        cu_q[i + 1] = cu_q[i] + q_lengths[i];
+        cu_kv[i + 1] = cu_kv[i] + kv_lengths[i];
+      }
+    }
+  }
+  if (tiles) {
+    if (tile_cap < (int32_t)items.size()) st = HBP_ERR_CAPACITY;
+    else
+      for (size_t j = 0; j < items.size(); ++j) tiles[j] = items[j].t;
+  }
+  return st;
+}
+
+extern "C" hbp_status hbp_cross_plan(const int32_t* q_lengths, const int32_t* kv_lengths, int32_t n_samples, int32_t tile_rows,
+                                     int32_t kind, int32_t* cu_q, int32_t* cu_kv, int32_t cu_cap, hbp_tile* tiles, int32_t tile_cap,
+                                     int32_t* n_tiles_out, int64_t* pairs_out) {
+  try {
+    return hbp_cross_plan_impl(q_lengths, kv_lengths, n_samples, tile_rows, kind, cu_q, cu_kv, cu_cap, tiles, tile_cap, n_tiles_out, pairs_out);
+  } catch (const std::bad_alloc&) {
+    return HBP_ERR_NO_MEMORY;
+  } catch (...) {
+    return HBP_ERR_INVALID_ARG;
+  }
+}

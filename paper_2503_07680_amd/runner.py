@@ -154,6 +154,73 @@ def _device(device) -> torch.device:
     return d if d.index is not None else torch.device(d.type, torch.cuda.current_device())
 
 
+class PackedCrossAttention:
+    """Cross attention of a pack: the query rows of sample i (``q_lengths[i]`` of them) attend to all of its
+    ``kv_lengths[i]`` keys; both sides packed, either may be empty for a sample.  Plans on the host, calls on the
+    device's current stream; like PackedAttention the object holds its outputs, the next call writes them again."""
+
+    def __init__(self, q_lengths: Sequence[int], kv_lengths: Sequence[int], n_q_heads: int, n_kv_heads: int,
+                 d_qk: int, d_v: int, softmax_scale: float = 0.0, device: str = "cuda:0"):
+        self.device = _device(device)
+        self.Hq, self.Hkv, self.d_qk, self.d_v = int(n_q_heads), int(n_kv_heads), int(d_qk), int(d_v)
+        self.Tq, self.Tk = int(sum(q_lengths)), int(sum(kv_lengths))
+        self.desc = B.CrossDesc(total_queries=self.Tq, total_keys=self.Tk, n_samples=len(q_lengths),
+                                n_q_heads=self.Hq, n_kv_heads=self.Hkv, d_qk=self.d_qk, d_v=self.d_v,
+                                softmax_scale=float(softmax_scale))
+        self.cu_q, self.cu_kv, q_tiles, self.pairs = B.hbp_cross_plan(
+            q_lengths, kv_lengths, B.hbp_cross_tile_rows(self.desc, B.HBP_FWD), B.HBP_TILES_QUERY)
+        _, _, kv_tiles, _ = B.hbp_cross_plan(
+            q_lengths, kv_lengths, B.hbp_cross_tile_rows(self.desc, B.HBP_BWD), B.HBP_TILES_KEY)
+        self.n_q_tiles, self.n_kv_tiles = len(q_tiles), len(kv_tiles)
+        # one copy; 16 bytes a tile, so both lists start on a tile's alignment
+        plan = torch.from_numpy(np.concatenate([q_tiles.ravel(), kv_tiles.ravel(), self.cu_q, self.cu_kv])).to(self.device)
+        self.q_tiles_dev, self.kv_tiles_dev, self.cu_q_dev, self.cu_kv_dev = plan.split(
+            [q_tiles.size, kv_tiles.size, self.cu_q.size, self.cu_kv.size])
+        dev, bf = self.device, torch.bfloat16
+        self.o = torch.empty((self.Tq, self.Hq, self.d_v), dtype=bf, device=dev)
+        self.lse = torch.empty((self.Hq, self.Tq), dtype=torch.float32, device=dev)
+        self.ws_fwd = torch.empty(B.hbp_cross_workspace_bytes(self.desc, B.HBP_FWD), dtype=torch.uint8, device=dev)
+        self.ws_bwd = self.dq = self.dk = self.dv = None
+
+    def _dense(self, name: str, t: torch.Tensor, shape) -> None:
+        _check(name, t, self.device, torch.bfloat16, shape)
+        if not t.is_contiguous():
+            raise ValueError("%s: a contiguous tensor is wanted" % name)
+
+    def _inputs(self, q, k, v) -> int:
+        self._dense("q", q, (self.Tq, self.Hq, self.d_qk))
+        self._dense("k", k, (self.Tk, self.Hkv, self.d_qk))
+        self._dense("v", v, (self.Tk, self.Hkv, self.d_v))
+        return int(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def forward(self, q, k, v):
+        """(o [Tq, Hq, d_v], lse [Hq, Tq]); rows of a sample without keys: zeros and -inf."""
+        stream = self._inputs(q, k, v)
+        with torch.cuda.device(self.device):
+            B.hbp_cross_attn_fwd(self.desc, q, k, v, self.cu_q_dev, self.cu_kv_dev, self.q_tiles_dev, self.n_q_tiles,
+                                 self.o, self.lse, self.ws_fwd, stream)
+        return self.o, self.lse
+
+    def alloc_backward(self):
+        if self.ws_bwd is None:
+            dev, bf = self.device, torch.bfloat16
+            self.ws_bwd = torch.empty(B.hbp_cross_workspace_bytes(self.desc, B.HBP_BWD), dtype=torch.uint8, device=dev)
+            self.dq = torch.empty((self.Tq, self.Hq, self.d_qk), dtype=bf, device=dev)
+            self.dk = torch.empty((self.Tk, self.Hkv, self.d_qk), dtype=bf, device=dev)
+            self.dv = torch.empty((self.Tk, self.Hkv, self.d_v), dtype=bf, device=dev)
+
+    def backward(self, q, k, v, d_o):
+        """(dq, dk, dv) of the last forward."""
+        stream = self._inputs(q, k, v)
+        self._dense("d_o", d_o, (self.Tq, self.Hq, self.d_v))
+        self.alloc_backward()
+        with torch.cuda.device(self.device):
+            B.hbp_cross_attn_bwd(self.desc, q, k, v, self.o, self.lse, d_o, self.cu_q_dev, self.cu_kv_dev,
+                                 self.q_tiles_dev, self.n_q_tiles, self.kv_tiles_dev, self.n_kv_tiles,
+                                 self.dq, self.dk, self.dv, self.ws_bwd, stream)
+        return self.dq, self.dk, self.dv
+
+
 class PackedEmbedding:
     """Token embedding of packs of ``total_tokens`` tokens, and its gradient.  Tokens are int32; one outside
     [0, vocab) is none: a row of zeros, no gradient.  Calls run on the device's current stream."""
@@ -170,7 +237,7 @@ class PackedEmbedding:
                                 row_type=_TYPES[out_type], scale=float(scale))
         self.ws_bytes = B.hbp_embed_bwd_workspace_bytes(self.desc)
         self.ws = None
-        self.out = torch.zeros((self.T, self.dim), dtype=out_type, device=self.device)
+        self.out = torch.empty((self.T, self.dim), dtype=out_type, device=self.device)
 
     def _rows(self, name: str, t: torch.Tensor, dtype, n: int) -> int:
         """Stride of [n, dim] rows in elements; overlapping or scattered rows are refused."""

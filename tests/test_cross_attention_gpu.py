@@ -1,0 +1,188 @@
+"""Cross attention, forward and backward, against its definition in 64 bits."""
+import pytest
+import torch
+
+from cross_util import check, exact, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def run(ql, kl, hq, hkv, d, e, x, scale=0.0):
+    from paper_2503_07680_amd.runner import PackedCrossAttention
+    a = PackedCrossAttention(ql, kl, hq, hkv, d, e, scale)
+    for t in (a.o, a.lse):
+        t.fill_(float("nan"))
+    o, lse = a.forward(*x[:3])
+    a.alloc_backward()
+    for t in (a.dq, a.dk, a.dv):
+        t.fill_(float("nan"))
+    dq, dk, dv = a.backward(*x)
+    return a, {"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+
+
+DIMS = [(64, 64), (128, 128), (192, 128)]
+LENGTHS = [
+    ([1], [1]), ([1], [64]), ([5], [33]), ([64], [65]), ([200], [31]), ([130], [129]),
+    ([1, 1, 1, 1], [700, 1, 63, 0]), ([0, 3, 70, 0], [9, 0, 257, 0]), ([300, 17], [0, 0]), ([0, 0], [40, 200]),
+    ([129, 64, 1, 255], [200, 96, 128, 32]), ([33, 400, 90], [1000, 2, 190]), ([700], [513]), ([20] * 70, [24] * 70),
+]
+
+
+@pytest.mark.parametrize("ql,kl", LENGTHS, ids=lambda v: "-".join(map(str, v[:4])) + ("x%d" % len(v) if len(v) > 4 else ""))
+@pytest.mark.parametrize("d,e", DIMS)
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (4, 1), (6, 2)])
+def test_lengths(ql, kl, d, e, hq, hkv):
+    print("case", ql[:4], kl[:4], d, hq, hkv, flush=True)
+    x = inputs(ql, kl, hq, hkv, d, e, sum(ql) + sum(kl) + d)
+    _, got = run(ql, kl, hq, hkv, d, e, x)
+    check(got, exact(ql, kl, *x), got)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (8, 1), (12, 3), (32, 8), (32, 1), (64, 1), (24, 1), (7, 7), (16, 2)])
+@pytest.mark.parametrize("d,e", DIMS)
+def test_heads(hq, hkv, d, e):
+    ql, kl = [37, 0, 90, 5], [150, 20, 77, 0]
+    x = inputs(ql, kl, hq, hkv, d, e, hq + d)
+    _, got = run(ql, kl, hq, hkv, d, e, x, scale=0.11)
+    check(got, exact(ql, kl, *x, scale=0.11), got)
+
+
+@pytest.mark.parametrize("ql,kl,hq,hkv", [([2000], [40], 8, 1), ([1500, 700], [100, 260], 4, 2), ([40], [3000], 4, 2), ([4096], [64], 2, 2)])
+@pytest.mark.parametrize("d,e", DIMS)
+def test_few_keys_or_few_rows(ql, kl, hq, hkv, d, e):
+    """Few key tiles under many rows (parts of the steps, added up) and few query tiles over many keys."""
+    x = inputs(ql, kl, hq, hkv, d, e, sum(ql) + d)
+    _, got = run(ql, kl, hq, hkv, d, e, x)
+    check(got, exact(ql, kl, *x), got)
+
+
+@pytest.mark.parametrize("d,e", DIMS)
+def test_peaked_and_growing_scores(d, e):
+    ql, kl = [150, 40], [400, 130]
+    q, k, v, d_o = inputs(ql, kl, 4, 2, d, e, 3)
+    k = (k.float() * torch.linspace(0.1, 6.0, sum(kl), device="cuda")[:, None, None]).to(torch.bfloat16)
+    _, got = run(ql, kl, 4, 2, d, e, (q, k, v, d_o))
+    check(got, exact(ql, kl, q, k, v, d_o), got)
+    k = (k.float() * -4).to(torch.bfloat16)
+    _, got = run(ql, kl, 4, 2, d, e, (q, k, v, d_o))
+    check(got, exact(ql, kl, q, k, v, d_o), got)
+
+
+def test_large_pack():
+    ql, kl = [900, 2100, 333, 1, 640], [1500, 700, 0, 4000, 1111]
+    x = inputs(ql, kl, 8, 2, 128, 128, 11)
+    a, got = run(ql, kl, 8, 2, 128, 128, x)
+    first = {n: t.clone() for n, t in got.items()}
+    check(got, exact(ql, kl, *x), got)
+    a.forward(*x[:3])
+    a.backward(*x)
+    assert all(torch.equal(first[n], t) for n, t in got.items())     # the same bits
+
+
+def test_samples_are_apart():
+    """What is not finite in one sample stays in it."""
+    ql, kl = [70, 130, 40], [100, 65, 30]
+    for d, e in DIMS:
+        q, k, v, d_o = inputs(ql, kl, 4, 2, d, e, 5)
+        _, clean = run(ql, kl, 4, 2, d, e, (q, k, v, d_o))
+        clean = {n: t.clone() for n, t in clean.items()}
+        for t, row in ((q, 100), (k, 120), (v, 130), (d_o, 90)):
+            t[row] = float("nan")
+        _, got = run(ql, kl, 4, 2, d, e, (q, k, v, d_o))
+        for n in ("o", "dq"):
+            assert torch.equal(got[n][:70], clean[n][:70]) and torch.equal(got[n][200:], clean[n][200:]), (n, d)
+        for n in ("dk", "dv"):
+            assert torch.equal(got[n][:100], clean[n][:100]) and torch.equal(got[n][165:], clean[n][165:]), (n, d)
+
+
+@pytest.mark.parametrize("d,e", DIMS)
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_strides(d, e, heads_first):
+    """Padded token strides (heads folded) and head-major tensors (not folded) through the C ABI; what lies between stays."""
+    import paper_2503_07680_amd as H
+    ql, kl, hq, hkv = [60, 31, 0, 200], [90, 0, 12, 140], 4, 2
+    tq, tk = sum(ql), sum(kl)
+    x = inputs(ql, kl, hq, hkv, d, e, 17)
+
+    def buffer(like, fill):
+        t, h, w = like.shape
+        if heads_first:
+            base = torch.full((h, t + 3, w + 8), fill, dtype=torch.bfloat16, device="cuda")
+            return base, base[:, :t, :w].permute(1, 0, 2)
+        base = torch.full((t + 1, h * (w + 8) + 16), fill, dtype=torch.bfloat16, device="cuda")
+        return base, base[:t, :h * (w + 8)].view(t, h, w + 8)[:, :, :w]
+
+    q, k, v, d_o = (buffer(t, float("nan"))[1] for t in x)
+    for a, b in zip((q, k, v, d_o), x):
+        a.copy_(b)
+    outs = {n: buffer(t, 7.0) for n, t in (("o", x[3]), ("dq", x[0]), ("dk", x[1]), ("dv", x[2]))}
+    s = {}
+    for n, t in (("q", q), ("k", k), ("v", v), ("o", d_o)):
+        s[n + "_stride_t"], s[n + "_stride_h"] = t.stride(0), t.stride(1)
+    desc = H.CrossDesc(total_queries=tq, total_keys=tk, n_samples=4, n_q_heads=hq, n_kv_heads=hkv, d_qk=d, d_v=e, **s)
+    assert H.hbp_cross_tile_rows(desc, H.HBP_FWD) == (256 if heads_first else 128)
+    cu_q, cu_kv, qt, _ = H.hbp_cross_plan(ql, kl, H.hbp_cross_tile_rows(desc, H.HBP_FWD), H.HBP_TILES_QUERY)
+    _, _, kt, _ = H.hbp_cross_plan(ql, kl, H.hbp_cross_tile_rows(desc, H.HBP_BWD), H.HBP_TILES_KEY)
+    dev = [torch.from_numpy(t).cuda() for t in (cu_q, cu_kv, qt, kt)]
+    lse = torch.full((hq, tq), 3.0, device="cuda")
+    ws = [torch.empty(H.hbp_cross_workspace_bytes(desc, w), dtype=torch.uint8, device="cuda") for w in (H.HBP_FWD, H.HBP_BWD)]
+    stream = torch.cuda.current_stream().cuda_stream
+    H.hbp_cross_attn_fwd(desc, q, k, v, dev[0], dev[1], dev[2], len(qt), outs["o"][1], lse, ws[0], stream)
+    H.hbp_cross_attn_bwd(desc, q, k, v, outs["o"][1], lse, d_o, dev[0], dev[1], dev[2], len(qt), dev[3], len(kt),
+                         outs["dq"][1], outs["dk"][1], outs["dv"][1], ws[1], stream)
+    got = dict({n: t for n, (_, t) in outs.items()}, lse=lse)
+    check(got, exact(ql, kl, *x), got)
+    for n, (base, view) in outs.items():
+        n_inside = view.numel()
+        view.fill_(7.0)
+        assert bool((base == 7.0).all()), n
+        assert base.numel() > n_inside
+
+
+def test_tiles_that_do_not_fit_are_skipped():
+    import paper_2503_07680_amd as H
+    from paper_2503_07680_amd.runner import PackedCrossAttention
+    ql, kl = [300, 20], [90, 200]
+    x = inputs(ql, kl, 4, 2, 128, 128, 4)
+    a = PackedCrossAttention(ql, kl, 4, 2, 128, 128)
+    a.forward(*x[:3])
+    a.backward(*x)
+    good = {n: getattr(a, n).clone() for n in ("o", "lse", "dq", "dk", "dv")}
+    bad = torch.tensor([[-1, 0, 0, 10], [2, 0, 0, 10], [0, 0, -5, 10], [0, 0, 290, 310], [1, 0, 0, 10], [0, 0, 0, 129], [0, 0, 10, 10],
+                        [1, 0, 2 ** 30, 2 ** 30 + 5]], dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    kv_bad = torch.tensor([[-1, 0, 0, 10], [2, 0, 0, 10], [0, 0, -5, 10], [0, 0, 80, 95], [1, 0, 0, 10], [1, 0, 90, 290], [0, 0, 10, 10]],
+                          dtype=torch.int32, device="cuda")
+    H.hbp_cross_attn_fwd(a.desc, *x[:3], a.cu_q_dev, a.cu_kv_dev, bad, len(bad), a.o, a.lse, a.ws_fwd, stream)
+    H.hbp_cross_attn_bwd(a.desc, *x[:3], a.o, a.lse, x[3], a.cu_q_dev, a.cu_kv_dev, bad, len(bad), kv_bad, len(kv_bad), a.dq, a.dk, a.dv, a.ws_bwd, stream)
+    assert all(torch.equal(getattr(a, n), t) for n, t in good.items())
+
+
+def test_captured_and_on_another_stream():
+    from paper_2503_07680_amd.runner import PackedCrossAttention
+    ql, kl = [300, 0, 64, 1200], [90, 20, 0, 70]
+    a = PackedCrossAttention(ql, kl, 8, 2, 128, 128)
+    b = PackedCrossAttention(ql, kl, 8, 2, 128, 128)
+    sets = [inputs(ql, kl, 8, 2, 128, 128, 40 + i) for i in range(3)]
+
+    def eager(s):
+        return [t.clone() for t in (*b.forward(*s[:3]), *b.backward(*s))]
+
+    want = [eager(s) for s in sets]
+    x = [t.clone() for t in sets[0]]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.forward(*x[:3])
+        a.backward(*x)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            out = (*a.forward(*x[:3]), *a.backward(*x))
+    torch.cuda.synchronize()
+    for i in (0, 1, 2, 1, 0):
+        for t, s in zip(x, sets[i]):
+            t.copy_(s)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(out, want[i])), i
+        eager(sets[(i + 1) % 3])
