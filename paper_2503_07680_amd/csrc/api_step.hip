@@ -123,7 +123,7 @@ extern "C" hbp_status hbp_cross_workspace_bytes(const hbp_cross_desc* desc, int3
   if (!bytes_out || (which != HBP_FWD && which != HBP_BWD)) return HBP_ERR_INVALID_ARG;
   const hbp_status st = check_cross(desc);
   if (st != HBP_OK) return st;
-  *bytes_out = which == HBP_FWD ? 0 : hbp::cross_bwd_layout(*desc).total;
+  *bytes_out = which == HBP_FWD ? hbp::cross_fwd_layout(*desc).total : hbp::cross_bwd_layout(*desc).total;
   return HBP_OK;
 }
 
@@ -133,8 +133,8 @@ extern "C" hbp_status hbp_cross_attn_fwd(const hbp_cross_desc* desc, const void*
   const hbp_status st = check_cross(desc);
   if (st != HBP_OK) return st;
   if (n_q_tiles < 0) return HBP_ERR_INVALID_ARG;
-  (void)workspace;
-  (void)workspace_bytes;
+  const hbp::CrossFwdLayout lay = hbp::cross_fwd_layout(*desc);
+  if (lay.total > 0 && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < lay.total)) return HBP_ERR_WORKSPACE;
   if (desc->total_queries == 0 || n_q_tiles == 0) return HBP_OK;
   if (!q || !o || !lse || !cu_q || !cu_kv || !q_tiles || (desc->total_keys > 0 && (!k || !v))) return HBP_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return HBP_ERR_INVALID_ARG;
@@ -160,6 +160,9 @@ extern "C" hbp_status hbp_cross_attn_fwd(const hbp_cross_desc* desc, const void*
   p.q_st = s.q_t; p.q_sh = s.q_h; p.k_st = s.k_t; p.k_sh = s.k_h;
   p.v_st = s.v_t; p.v_sh = s.v_h; p.o_st = s.o_t; p.o_sh = s.o_h;
   p.scale_log2 = scale_of(desc) * kLog2e;
+  p.parts = lay.parts;
+  p.o_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.o_off);
+  p.ml_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.ml_off);
   return hbp::launch_cross_fwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
 }
 

@@ -13,6 +13,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWave = 64;
 constexpr int kThreads = 256;  // 4 wavefronts per workgroup, one per SIMD
@@ -770,6 +771,8 @@ struct FwdParams {
   // the number of folded groups that read one kv head, and a "head" of an item is such a group.
   const int32_t* cu_kv;
   int32_t Tk, fold_log2;
+  int32_t parts;           // a sample's keys are dealt out in so many; from two on:
+  float *o_part, *ml_part; // [part][folded group][token][F] of [d_v], and of {reference, row sum}
 };
 
 struct BwdParams {

@@ -40,6 +40,32 @@ inline int cross_parts(const hbp_cross_desc& d) {
   return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
 }
 
+// In how many parts the forward deals out the keys of a query tile: where there are few tiles (tokens of generation, a few
+// learned queries) a workgroup for each and every key in turn leaves the chip idle.
+inline int cross_fwd_parts(const hbp_cross_desc& d) {
+  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return 1;
+  const int l = cross_fold_log2(d);
+  const int64_t full = (((int64_t)d.total_queries << l) + kCrossRows - 1) / kCrossRows, some = d.n_samples < d.total_queries ? d.n_samples : d.total_queries;
+  const int64_t items = (full > some ? full : some) * (d.n_q_heads >> l), keys = d.total_keys / d.n_samples;
+  int64_t parts = 2048 / items;
+  if (parts > keys / 128) parts = keys / 128;
+  return (int)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+}
+struct CrossFwdLayout {
+  size_t o_off, ml_off, total;
+  int parts;
+};
+inline CrossFwdLayout cross_fwd_layout(const hbp_cross_desc& d) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  CrossFwdLayout l;
+  l.parts = cross_fwd_parts(d);
+  const size_t rows = l.parts > 1 ? (size_t)l.parts * d.n_q_heads * d.total_queries : 0;
+  l.o_off = 0;
+  l.ml_off = up(rows * d.d_v * 4);
+  l.total = l.ml_off + up(rows * 8);
+  return l;
+}
+
 struct CrossBwdLayout {
   size_t d_off, lse2_off, dk_part_off, dv_part_off, total;
   int parts;

@@ -319,7 +319,8 @@ __device__ __forceinline__ FwdArgs* fwd_args() {
 //
 // CROSS: cross attention (see hbp_cross_attn_fwd).  A tile's rows are the folded rows of its tokens (see Fold), TP * 128 of
 // them a workgroup; every row sees all keys of its sample, so all wavefronts have the same blocks and the last one is masked
-// where the keys end.  Always DIRECT.
+// where the keys end.  Always DIRECT.  With p.parts > 1 the sample's keys are dealt out in so many parts of whole tiles, the
+// grid's second dimension, and each leaves its O, not divided, its reference and its row sum to cross_join_kernel.
 template <int DQK, int DV, int HP, int TP, bool DIRECT, bool CROSS = false>
 __device__ __forceinline__ void fwd_items() {
   static_assert(HP * TP <= 2, "eight wavefronts per compute unit");
@@ -374,7 +375,7 @@ __device__ __forceinline__ void fwd_items() {
     int tile_idx, h;
     if constexpr (DIRECT) {
       tile_idx = blockIdx.z;
-      h = blockIdx.x * gridDim.y + blockIdx.y;
+      h = CROSS ? blockIdx.x : blockIdx.x * gridDim.y + blockIdx.y;
     } else {
       const WorkQueues wq{p.counter, p.n_tiles, p.Hkv * p.n_split, p.g / HP / p.n_split};
       if (!next_item<true>(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, h)) break;
@@ -403,6 +404,11 @@ __device__ __forceinline__ void fwd_items() {
         ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= (BM << halves) >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
              BM * half < (tl.row_end - tl.row_begin) << p.fold_log2;
+        if (ok && p.parts > 1) {  // this workgroup's part of the keys
+          const int per = ((ks1 - ks0 + p.parts - 1) / p.parts + BN - 1) / BN * BN, from = min((int64_t)per * blockIdx.y, (int64_t)(ks1 - ks0));
+          ks1 = min(ks1 - ks0 - from, per) + ks0 + from;
+          ks0 += from;
+        }
       }
     } else if (ok) {
       // tiles start a multiple of 32 rows into their sample: each wave then has exactly one key
@@ -604,6 +610,20 @@ __device__ __forceinline__ void fwd_items() {
         const bool row_valid = l32 < rows_left;
         if constexpr (CROSS) {
           const int f0 = r0 + 32 * rw, f = f0 + l32;
+          if (p.parts > 1) {
+            const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2;
+            const int64_t row = blockIdx.y * rows + (((int64_t)h * p.T + tl.row_begin) << p.fold_log2) + f;
+            if (row_valid) {
+              float* op = p.o_part + row * DV + 4 * hh;
+#pragma unroll
+              for (int eb = 0; eb < NEB; ++eb)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                  *(f32x4*)(op + 32 * eb + 8 * b) = f32x4{w.oacc[eb][4 * b], w.oacc[eb][4 * b + 1], w.oacc[eb][4 * b + 2], w.oacc[eb][4 * b + 3]};
+              if (hh == 0) *(f32x2*)(p.ml_part + 2 * row) = f32x2{n_keys == 0 ? -INFINITY : w.m_run, l_tot};
+            }
+            break;
+          }
           const int64_t token = tl.row_begin + (f0 >> p.fold_log2);
           uint16_t* const rows = p.o + token * p.o_st + (int64_t)(h << p.fold_log2) * p.o_sh;
           const Fold fold{p.fold_log2, (uint32_t)p.o_st * 2, (uint32_t)p.o_sh * 2};
@@ -666,6 +686,51 @@ __global__ __launch_bounds__(kThreads * HP * TP, 2 / (HP * TP)) void fwd_direct_
 template <int DQK, int DV, int TP>
 __global__ __launch_bounds__(kThreads * TP, 2 / TP) void cross_forward_kernel(const FwdParams) {
   fwd_items<DQK, DV, 1, TP, true, true>();
+}
+
+// O and LSE of a tile's rows from their parts: with m the largest of the references m_i, O = sum 2^(m_i - m) O_i / l and
+// LSE = (m + log2 l) ln 2, l = sum 2^(m_i - m) l_i.  DV / 4 lanes a row; bound by reading the parts once.  Grid: folded groups,
+// kJoinShares workgroups, tiles.
+constexpr int kJoinShares = 4;
+template <int DV>
+__global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p) {
+  constexpr int LPR = DV / 4;
+  const hbp_tile tl = p.tiles[blockIdx.z];
+  if (tl.sample < 0 || tl.sample >= p.n_samples) return;
+  const int s0 = p.cu[tl.sample], s1 = p.cu[tl.sample + 1], ks0 = p.cu_kv[tl.sample], ks1 = p.cu_kv[tl.sample + 1];
+  // the tiles that the forward takes
+  if (!(s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+        tl.row_end - tl.row_begin <= 256 >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk))
+    return;
+  const int n_rows = (tl.row_end - tl.row_begin) << p.fold_log2, x = threadIdx.x % LPR;
+  const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
+  for (int f = blockIdx.y * (kThreads / LPR) + threadIdx.x / LPR; f < n_rows; f += kJoinShares * (kThreads / LPR)) {
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    for (int at = 0; at < p.parts; at += 4) {  // four parts' loads under way
+      f32x2 ml[4];
+      f32x4 o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = min(at + i, p.parts - 1) * rows + row0 + f;
+        ml[i] = *(const f32x2*)(p.ml_part + 2 * r);
+        o[i] = *(const f32x4*)(p.o_part + r * DV + 4 * x);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (at + i >= p.parts || ml[i][0] == -INFINITY) continue;  // a part without keys
+        const float top = fmaxf(m, ml[i][0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[i][0] - top);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + o[i][j] * b;
+        l = l * a + ml[i][1] * b;
+        m = top;
+      }
+    }
+    const int64_t h = ((int64_t)blockIdx.x << p.fold_log2) + (f & ((1 << p.fold_log2) - 1)), token = tl.row_begin + (f >> p.fold_log2);
+    const float inv = m == -INFINITY ? 0.f : 1.f / l;
+    *(u32x2*)(p.o + token * p.o_st + h * p.o_sh + 4 * x) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+    if (x == 0) p.lse[h * p.T + token] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
 }
 
 __global__ void zero_counters_kernel(int32_t* c) {
@@ -746,18 +811,22 @@ static int launch_cross_fwd_t(FwdParams p, hipStream_t s) {
     FwdParams part = p;
     part.tiles += at;
     part.n_tiles = (p.n_tiles - at < kMost ? p.n_tiles - at : kMost) << p.halves;
-    hipLaunchKernelGGL((cross_forward_kernel<DQK, DV, TP>), dim3((unsigned)(p.Hkv * p.g), 1, (unsigned)part.n_tiles), dim3(kThreads * TP), lds_bytes, s, part);
-    const hipError_t e = hipGetLastError();
+    hipLaunchKernelGGL((cross_forward_kernel<DQK, DV, TP>), dim3((unsigned)(p.Hkv * p.g), (unsigned)p.parts, (unsigned)part.n_tiles), dim3(kThreads * TP), lds_bytes, s, part);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
+    if (p.parts > 1) {
+      hipLaunchKernelGGL((cross_join_kernel<DV>), dim3((unsigned)(p.Hkv * p.g), kJoinShares, (unsigned)(part.n_tiles >> p.halves)), dim3(kThreads), 0, s, part);
+      e = hipGetLastError();
+      if (e != hipSuccess) return (int)e;
+    }
   }
   return 0;
 }
 template <int DQK, int DV>
 static int launch_cross_fwd_d(const FwdParams& p, hipStream_t s) {
   // a 256-row tile a workgroup of eight wavefronts, or, where those would not fill the chip, half of one
-  const bool halves = FwdLds<DQK, DV, 4>::kStaged && (int64_t)p.n_tiles * p.Hkv * p.g <= 2 * kNumCU;
   if constexpr (FwdLds<DQK, DV, 4>::kStaged) {
-    if (halves) return launch_cross_fwd_t<DQK, DV, 1>(p, s);
+    if ((int64_t)p.n_tiles * p.Hkv * p.g * p.parts <= 2 * kNumCU || p.parts > 1) return launch_cross_fwd_t<DQK, DV, 1>(p, s);
   }
   return launch_cross_fwd_t<DQK, DV, 2>(p, s);
 }

@@ -47,7 +47,9 @@ def test_heads(hq, hkv, d, e):
     check(got, exact(ql, kl, *x, scale=0.11), got)
 
 
-@pytest.mark.parametrize("ql,kl,hq,hkv", [([2000], [40], 8, 1), ([1500, 700], [100, 260], 4, 2), ([40], [3000], 4, 2), ([4096], [64], 2, 2)])
+@pytest.mark.parametrize("ql,kl,hq,hkv", [([2000], [40], 8, 1), ([1500, 700], [100, 260], 4, 2), ([40], [3000], 4, 2), ([4096], [64], 2, 2),
+                                           ([1], [20000], 8, 2), ([1] * 9, [900, 3, 4000, 0, 64, 1000, 129, 2500, 700], 8, 2),
+                                           ([3, 0, 300, 1], [2000, 50, 1500, 0], 6, 2), ([64, 64], [5000, 300], 4, 4)])
 @pytest.mark.parametrize("d,e", DIMS)
 def test_few_keys_or_few_rows(ql, kl, hq, hkv, d, e):
     """Few key tiles under many rows (parts of the steps, added up) and few query tiles over many keys."""
@@ -139,10 +141,13 @@ def test_strides(d, e, heads_first):
         assert base.numel() > n_inside
 
 
-def test_tiles_that_do_not_fit_are_skipped():
+@pytest.mark.parametrize("kl", [[90, 200], [2000, 1500]])     # keys in one part, and in several
+def test_tiles_that_do_not_fit_are_skipped(kl):
     import paper_2503_07680_amd as H
     from paper_2503_07680_amd.runner import PackedCrossAttention
-    ql, kl = [300, 20], [90, 200]
+    ql = [300, 20]
+    assert (H.hbp_cross_workspace_bytes(H.CrossDesc(total_queries=320, total_keys=sum(kl), n_samples=2, n_q_heads=4, n_kv_heads=2,
+                                                    d_qk=128, d_v=128), H.HBP_FWD) > 0) == (kl[0] == 2000)
     x = inputs(ql, kl, 4, 2, 128, 128, 4)
     a = PackedCrossAttention(ql, kl, 4, 2, 128, 128)
     a.forward(*x[:3])
@@ -151,8 +156,8 @@ def test_tiles_that_do_not_fit_are_skipped():
     bad = torch.tensor([[-1, 0, 0, 10], [2, 0, 0, 10], [0, 0, -5, 10], [0, 0, 290, 310], [1, 0, 0, 10], [0, 0, 0, 129], [0, 0, 10, 10],
                         [1, 0, 2 ** 30, 2 ** 30 + 5]], dtype=torch.int32, device="cuda")
     stream = torch.cuda.current_stream().cuda_stream
-    kv_bad = torch.tensor([[-1, 0, 0, 10], [2, 0, 0, 10], [0, 0, -5, 10], [0, 0, 80, 95], [1, 0, 0, 10], [1, 0, 90, 290], [0, 0, 10, 10]],
-                          dtype=torch.int32, device="cuda")
+    kv_bad = torch.tensor([[-1, 0, 0, 10], [2, 0, 0, 10], [0, 0, -5, 10], [0, 0, kl[0] - 10, kl[0] + 5], [1, 0, 0, 10],
+                           [1, 0, kl[0], kl[0] + 129], [0, 0, 10, 10]], dtype=torch.int32, device="cuda")
     H.hbp_cross_attn_fwd(a.desc, *x[:3], a.cu_q_dev, a.cu_kv_dev, bad, len(bad), a.o, a.lse, a.ws_fwd, stream)
     H.hbp_cross_attn_bwd(a.desc, *x[:3], a.o, a.lse, x[3], a.cu_q_dev, a.cu_kv_dev, bad, len(bad), kv_bad, len(kv_bad), a.dq, a.dk, a.dv, a.ws_bwd, stream)
     assert all(torch.equal(getattr(a, n), t) for n, t in good.items())

@@ -115,6 +115,15 @@ def test_calls():
     assert bwd(q_tiles=0, kv_tiles=0, cu_q=None) == 0
 
 
+def test_the_forwards_workspace():
+    lib, few, many = H.load_library(), desc(total_queries=2, total_keys=6000), desc(total_queries=60000, total_keys=6000)
+    assert H.hbp_cross_workspace_bytes(many, H.HBP_FWD) == 0          # tiles enough: the keys in one part
+    need = H.hbp_cross_workspace_bytes(few, H.HBP_FWD)
+    assert need > 2 * 8 * 128 * 4
+    for ws, size in ((None, need), (FAKE + 16, need), (FAKE, need - 1)):
+        assert lib.hbp_cross_attn_fwd(ctypes.byref(few), *[FAKE] * 6, 1, FAKE, FAKE, ws, size, None) == 5
+
+
 def test_nothing_to_attend_or_to_ask():
     for kw in (dict(total_queries=0), dict(total_keys=0), dict(total_queries=0, total_keys=0, n_samples=0)):
         d = desc(**kw)
