@@ -219,6 +219,8 @@ extern "C" hbp_status hbp_cross_attn_bwd(const hbp_cross_desc* desc, const void*
   p.n_split_dq = 1;
   p.dk_part = reinterpret_cast<float*>(ws + lay.dk_part_off);
   p.dv_part = reinterpret_cast<float*>(ws + lay.dv_part_off);
+  p.dq_parts = lay.dq_parts;
+  p.dq_part = reinterpret_cast<float*>(ws + lay.dq_part_off);
   return hbp::launch_cross_bwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
 }
 

@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "cross_rules.hpp"
 
 namespace hbp {
 
@@ -109,11 +110,13 @@ struct DqLds {
 };
 
 //
-// CROSS: cross attention.  An item is 128 folded rows (see Fold) of a query tile for one folded group of heads; every row sees
-// all keys of its sample.
+// CROSS: cross attention.  An item is 128 folded rows (see Fold) of a query tile for one folded group of heads, which the place
+// in the grid names; HALVES = 2: the tile's 256, on shared tiles, item `block` of the launch.  Every row sees all keys of its
+// sample; with p.dq_parts > 1 these are dealt out in so many parts of whole key tiles, and the parts' sums of dQ are added up by
+// cross_reduce_dq_kernel.
 template <int DQK, int DV, int HALVES = 1, bool SHARED = false, bool DIRECT = HALVES == 2, bool CROSS = false>
 __device__ __forceinline__ void dq_items(int block) {
-  static_assert(!CROSS || (DIRECT && HALVES == 1), "heads are folded into rows");
+  static_assert(!CROSS || (DIRECT && SHARED == (HALVES == 2)), "heads are folded into rows");
   using Lds = DqLds<DQK, DV, HALVES, SHARED>;
   constexpr int BM = 128, BN = 64;
   constexpr int KRB = DQK * 2, VRB = DV * 2;
@@ -174,10 +177,19 @@ __device__ __forceinline__ void dq_items(int block) {
   for (;;) {
     const BwdArgs& p = *bwd_args<!DIRECT>();
     const WorkQueues wq{p.counter_dq, p.n_q_tiles, p.Hkv * p.n_split_dq, quotient(p.g / (SHARED ? 2 : 1), p.n_split_dq)};
-    int tile_idx, h;
+    int tile_idx, h, key_part = 0;
     if constexpr (CROSS) {
-      tile_idx = blockIdx.z;
-      h = blockIdx.x;
+      const int groups = p.Hkv * p.g;
+      if constexpr (HALVES == 1) {
+        tile_idx = blockIdx.z;
+        h = blockIdx.x;
+        key_part = blockIdx.y >> 1;
+      } else {
+        const int of_part = p.n_q_tiles * groups;
+        key_part = quotient(block, of_part);
+        tile_idx = quotient(block - key_part * of_part, groups);
+        h = block - key_part * of_part - tile_idx * groups;
+      }
     } else if constexpr (!DIRECT) {
       if (!next_item(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, h)) break;
     } else {
@@ -190,15 +202,20 @@ __device__ __forceinline__ void dq_items(int block) {
 
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.q_tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
     int ks0 = 0, ks1 = 0;
+    bool ok;
+    if constexpr (CROSS) ok = load_tile(p.q_tiles, tile_idx, p.cu, p.cu_kv, p.n_samples, lane, tl, s0, s1, ks0, ks1);
+    else ok = load_tile(p.q_tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
     if constexpr (CROSS) {
       if (ok) {
-        ks0 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample]);
-        ks1 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample + 1]);
         ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= 2 * BM >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
-             BM * (int)blockIdx.y < (tl.row_end - tl.row_begin) << p.fold_log2;
+             (HALVES == 2 || BM * (int)(blockIdx.y & 1) < (tl.row_end - tl.row_begin) << p.fold_log2);
+        if (ok && p.dq_parts > 1) {
+          const int n = ks1 - ks0, per = ((n + p.dq_parts - 1) / p.dq_parts + BN - 1) / BN * BN, from = min((int64_t)per * key_part, (int64_t)n);
+          ks1 = ks0 + from + min(n - from, per);
+          ks0 += from;
+        }
       }
     } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
@@ -206,7 +223,7 @@ __device__ __forceinline__ void dq_items(int block) {
     }
     if (ok) {
       // CROSS: rows of the tile, folded, from 0 on
-      const int r0 = CROSS ? BM * (int)blockIdx.y : tl.row_begin;
+      const int r0 = CROSS ? BM * (HALVES == 2 ? half : (int)(blockIdx.y & 1)) : tl.row_begin;
       const int r1 = CROSS ? min(r0 + BM, (tl.row_end - tl.row_begin) << p.fold_log2) : tl.row_end;
       const bool has_head = HALVES == 1 || SHARED || h < p.Hq;  // an odd number of heads: the last pair has one
       if (!has_head) h = p.Hq - 1;
@@ -466,7 +483,18 @@ __device__ __forceinline__ void dq_items(int block) {
       if (CROSS && nkt == 0) wait_async_loads();  // no tile has waited for the rows
       __syncthreads();  // the tiles are no longer read
       race_fence();
-      if (wave_active) {
+      if (CROSS && p.dq_parts > 1) {
+        if (row_valid) {
+          const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2;
+          float* out = p.dq_part + (key_part * rows + (((int64_t)h * p.T + tl.row_begin) << p.fold_log2) + my_row) * DQK + 4 * hh;
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              *(f32x4*)(out + 32 * db + 8 * b) = f32x4{dqacc[db][4 * b] * p.scale, dqacc[db][4 * b + 1] * p.scale,
+                                                         dqacc[db][4 * b + 2] * p.scale, dqacc[db][4 * b + 3] * p.scale};
+        }
+      } else if (wave_active) {
         const uint32_t at = lds_all + wave_in_wg * Lds::UNIT;
         RowStage<DQK>::put(at, lane, dqacc, p.scale);
         if constexpr (CROSS) {
@@ -586,8 +614,9 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
     const int g_item = CROSS ? p.g : quotient(p.g, p.n_split);
     int tile_idx, vh;
     if constexpr (CROSS) {
-      tile_idx = blockIdx.z;
-      vh = blockIdx.x;
+      const int groups = p.Hkv * p.n_split;
+      tile_idx = block < 0 ? (int)blockIdx.z : quotient(block, groups);  // block < 0: by the place in the grid
+      vh = block < 0 ? (int)blockIdx.x : block - tile_idx * groups;
     } else if constexpr (DIRECT) {
       const Taken tk = direct_item_inline(wq.n_tiles, wq.Hkv, 1, 0, 0, block);
       tile_idx = __builtin_amdgcn_readfirstlane(tk.tile_idx);
@@ -601,12 +630,12 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
 
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.tiles, tile_idx, CROSS ? p.cu_kv : p.cu, p.n_samples, lane, tl, s0, s1);
     int qs0 = 0, qs1 = 0;
+    bool ok;
+    if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx, p.cu_kv, p.cu, p.n_samples, lane, tl, s0, s1, qs0, qs1);
+    else ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
     if constexpr (CROSS) {
       if (ok) {
-        qs0 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample]);
-        qs1 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample + 1]);
         ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
       }
@@ -1101,8 +1130,9 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
     const int g_item = CROSS ? p.g : quotient(p.g, p.n_split);
     int tile_idx, vh;
     if constexpr (CROSS) {
-      tile_idx = blockIdx.z;
-      vh = blockIdx.x;
+      const int groups = p.Hkv * p.n_split;
+      tile_idx = block < 0 ? (int)blockIdx.z : quotient(block, groups);  // block < 0: by the place in the grid
+      vh = block < 0 ? (int)blockIdx.x : block - tile_idx * groups;
     } else if constexpr (DIRECT) {
       const Taken tk = direct_item_inline(wq.n_tiles, wq.Hkv, 1, 0, 0, block);
       tile_idx = __builtin_amdgcn_readfirstlane(tk.tile_idx);
@@ -1116,12 +1146,12 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
 
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.tiles, tile_idx, CROSS ? p.cu_kv : p.cu, p.n_samples, lane, tl, s0, s1);
     int qs0 = 0, qs1 = 0;
+    bool ok;
+    if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx, p.cu_kv, p.cu, p.n_samples, lane, tl, s0, s1, qs0, qs1);
+    else ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
     if constexpr (CROSS) {
       if (ok) {
-        qs0 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample]);
-        qs1 = __builtin_amdgcn_readfirstlane(p.cu[tl.sample + 1]);
         ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
       }
@@ -1723,11 +1753,47 @@ __global__ __launch_bounds__(kThreads, DQK <= 128 ? 2 : 1) void cross_dq_kernel(
 }
 template <int DQK, int DV>
 __global__ __launch_bounds__(2 * kThreads, 2) void cross_dkdv_eight_kernel(const BwdParams) {
-  dkdv8_items<DQK, DV, true, true>(0, 1);
+  dkdv8_items<DQK, DV, true, true>(-1, 1);
 }
 template <int DQK, int DV>
 __global__ __launch_bounds__(kThreads, 1) void cross_dkdv_four_kernel(const BwdParams) {
-  dkdv_items<DQK, DV, true, true>(0, 1);
+  dkdv_items<DQK, DV, true, true>(-1, 1);
+}
+// dK/dV and dQ in one launch (see cross_one_launch), the kind with the longer items first.
+template <int DQK, int DV>
+__global__ __launch_bounds__(2 * kThreads, 2) void cross_both_eight_kernel(const BwdParams, int n_dkdv, int n_dq, int dq_first) {
+  const int block = blockIdx.x;
+  if (dq_first ? block >= n_dq : block < n_dkdv) dkdv8_items<DQK, DV, true, true>(dq_first ? block - n_dq : block, 1);
+  else dq_items<DQK, DV, 2, true, true, true>(dq_first ? block : block - n_dkdv);
+}
+
+// dQ of a tile's rows from the parts' sums, in the parts' order.  DQK / 4 lanes a row; bound by reading the parts once.  Grid:
+// folded groups, shares of the rows, tiles.
+template <int DQK>
+__global__ __launch_bounds__(kThreads) void cross_reduce_dq_kernel(const BwdParams p) {
+  constexpr int LPR = DQK / 4;
+  const hbp_tile tl = p.q_tiles[blockIdx.z];
+  if (tl.sample < 0 || tl.sample >= p.n_samples) return;
+  const int s0 = p.cu[tl.sample], s1 = p.cu[tl.sample + 1], ks0 = p.cu_kv[tl.sample], ks1 = p.cu_kv[tl.sample + 1];
+  if (!(s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
+        tl.row_end - tl.row_begin <= 256 >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk))
+    return;
+  const int n_units = ((tl.row_end - tl.row_begin) << p.fold_log2) * LPR;
+  const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
+  for (int u = blockIdx.y * kThreads + threadIdx.x; u < n_units; u += gridDim.y * kThreads) {
+    const int f = u / LPR, x = u - f * LPR;
+    const float* src = p.dq_part + (row0 + f) * DQK + 4 * x;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int at = 0; at < p.dq_parts; at += 8) {  // eight parts' loads under way
+      f32x4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = at + i < p.dq_parts ? *(const f32x4*)(src + (at + i) * rows * DQK) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc += v[i];
+    }
+    const int64_t h = ((int64_t)blockIdx.x << p.fold_log2) + (f & ((1 << p.fold_log2) - 1)), token = tl.row_begin + (f >> p.fold_log2);
+    *(u32x2*)(p.dq + token * p.q_st + h * p.q_sh + 4 * x) = u32x2{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3])};
+  }
 }
 
 constexpr int kCrossMostTiles = 65535;  // of one launch: the grid's third dimension
@@ -1758,7 +1824,25 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
-  for (int at = 0; at < p.n_tiles; at += kCrossMostTiles) {
+  bool one = false;
+  if constexpr (kEight) {
+    const int64_t n_dkdv = (int64_t)p.n_tiles * p.Hkv * p.n_split, n_dq = (int64_t)p.n_q_tiles * p.Hkv * p.g * p.dq_parts;
+    one = cross_one_launch(n_dkdv, n_dq);
+    if (one) {
+      constexpr int lds_both_dq = DqLds<DQK, DV, 2, true>::BYTES, lds = lds_both_dq > lds_dkdv ? lds_both_dq : lds_dkdv;
+      static bool both_set = false;
+      if (!both_set) {
+        e = hipFuncSetAttribute((const void*)cross_both_eight_kernel<DQK, DV>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return (int)e;
+        both_set = true;
+      }
+      hipLaunchKernelGGL((cross_both_eight_kernel<DQK, DV>), dim3((unsigned)(n_dkdv + n_dq)), dim3(2 * kThreads), lds, s, p, (int)n_dkdv, (int)n_dq,
+                         (int)cross_dq_first(p.T, p.Tk, (p.Hq / p.Hkv), p.n_split, p.dq_parts));
+      e = hipGetLastError();
+      if (e != hipSuccess) return (int)e;
+    }
+  }
+  for (int at = 0; at < p.n_tiles && !one; at += kCrossMostTiles) {
     BwdParams part = p;
     part.tiles += at;
     part.n_tiles = p.n_tiles - at < kCrossMostTiles ? p.n_tiles - at : kCrossMostTiles;
@@ -1775,11 +1859,19 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
-  for (int at = 0; at < p.n_q_tiles; at += kCrossMostTiles) {
+  for (int at = 0; at < p.n_q_tiles && !one; at += kCrossMostTiles) {
     BwdParams part = p;
     part.q_tiles += at;
     part.n_q_tiles = p.n_q_tiles - at < kCrossMostTiles ? p.n_q_tiles - at : kCrossMostTiles;
-    hipLaunchKernelGGL((cross_dq_kernel<DQK, DV>), dim3((unsigned)(p.Hkv * p.g), 2, (unsigned)part.n_q_tiles), dim3(kThreads), lds_dq, s, part);
+    hipLaunchKernelGGL((cross_dq_kernel<DQK, DV>), dim3((unsigned)(p.Hkv * p.g), 2 * (unsigned)p.dq_parts, (unsigned)part.n_q_tiles), dim3(kThreads), lds_dq, s, part);
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  for (int at = 0; at < p.n_q_tiles && p.dq_parts > 1; at += kCrossMostTiles) {
+    BwdParams part = p;
+    part.q_tiles += at;
+    const int n = p.n_q_tiles - at < kCrossMostTiles ? p.n_q_tiles - at : kCrossMostTiles;
+    hipLaunchKernelGGL((cross_reduce_dq_kernel<DQK>), dim3((unsigned)(p.Hkv * p.g), cross_join_shares(p.Hkv * p.g, n), (unsigned)n), dim3(kThreads), 0, s, part);
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }

@@ -754,6 +754,24 @@ __device__ __forceinline__ bool load_tile(const hbp_tile* tiles, int idx, const 
   return true;
 }
 
+// The same for cross attention, with the bounds of the sample's other side, o0 and o1, read beside its own.
+__device__ __forceinline__ bool load_tile(const hbp_tile* tiles, int idx, const int32_t* cu, const int32_t* cu_other, int n_samples, int lane,
+                                          hbp_tile& tl, int& s0, int& s1, int& o0, int& o1) {
+  asm volatile("" : "+v"(lane));
+  const int other = cu_other[min(lane, n_samples)];
+  const bool ok = load_tile(tiles, idx, cu, n_samples, lane, tl, s0, s1);
+  o0 = o1 = 0;
+  if (!ok) return false;
+  if (n_samples < kWave) {
+    o0 = __builtin_amdgcn_readlane(other, tl.sample);
+    o1 = __builtin_amdgcn_readlane(other, tl.sample + 1);
+  } else {
+    o0 = __builtin_amdgcn_readfirstlane(cu_other[tl.sample]);
+    o1 = __builtin_amdgcn_readfirstlane(cu_other[tl.sample + 1]);
+  }
+  return true;
+}
+
 struct FwdParams {
   const uint16_t *q, *k, *v;
   uint16_t* o;
@@ -799,6 +817,8 @@ struct BwdParams {
   // steps over the query rows (see cross_dkdv).
   const int32_t* cu_kv;
   int32_t Tk, fold_log2;
+  int32_t dq_parts;  // a sample's keys are dealt out in so many for dQ; from two on:
+  float* dq_part;    // [part][folded group][token][F][d_qk]
 };
 
 struct CeParams {  // packed cross-entropy

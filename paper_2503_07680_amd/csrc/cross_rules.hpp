@@ -29,27 +29,56 @@ inline int cross_fold_log2(const hbp_cross_desc& d) {
 }
 constexpr int kCrossRows = 256, kCrossKeys = 128;  // folded rows of a query tile, keys of a key tile
 
-// In how many parts the steps over a key tile's query rows are dealt out, each an item of its own (their sums of dK and dV are
-// added up by the reduce kernel): as many as give every compute unit two, of at least 8 steps in the mean.
+// In how many parts the steps over a key tile's query rows (64 of them a step) are dealt out, each an item of its own, whose sums
+// of dK and dV are added up by the reduce kernel: where there are fewer than some 192 key tiles (a tile and a kv head each), of
+// six steps at least.  Backward, us, in one part -> as here (best of 1 to 32): 4407 queries, 113 keys, 32/8 heads of 128: 375 -> 82
+// (75); 3458, 60, 8/1: 370 -> 32.7 (32.7); 9588, 1356, 8/1: 1524 -> 196 (192); 9682, 963, 32/8: 857 -> 508 (508); 4 samples of
+// 1240, 150, 32/8: 156 -> 85 (82); 16 of 530, 860, 8/1: 202 -> 137 (137); 4 of 1080, 105, 24/24: 55.8 -> 63.8 (55.8); 280 tiles of 29
+// steps: 79.5 in one part, 95.4 in two.
 inline int cross_parts(const hbp_cross_desc& d) {
   if (d.total_keys == 0 || d.total_queries == 0) return 1;
   const int64_t items = ((int64_t)d.total_keys + kCrossKeys - 1) / kCrossKeys * d.n_kv_heads;
   const int64_t steps = (int64_t)d.total_queries * (d.n_q_heads / d.n_kv_heads) / (d.n_samples > 0 ? d.n_samples : 1) / 64;
-  int64_t parts = (512 + items - 1) / items;
-  if (parts > steps / 8) parts = steps / 8;
-  return (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+  int64_t parts = (192 + items / 2) / items;
+  if (parts > steps / 6) parts = steps / 6;
+  return (int)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+}
+
+// Query tiles of the mean sample, as far as the descriptor tells, for all folded groups of heads; rows of one; key tiles (of 64).
+struct CrossTiles {
+  int64_t items, rows, key_tiles;
+};
+inline CrossTiles cross_tiles(const hbp_cross_desc& d) {
+  const int l = cross_fold_log2(d);
+  const int64_t rows = (int64_t)d.total_queries << l, full = (rows + kCrossRows - 1) / kCrossRows;
+  const int64_t some = d.n_samples < d.total_queries ? d.n_samples : d.total_queries, tiles = full > some ? full : some;
+  return {tiles * (d.n_q_heads >> l), rows / tiles, d.total_keys / d.n_samples / 64};
 }
 
 // In how many parts the forward deals out the keys of a query tile: where there are few tiles (tokens of generation, a few
-// learned queries) a workgroup for each and every key in turn leaves the chip idle.
+// learned queries) a workgroup for each, and every key in turn, leaves the chip idle.  A tile of few rows is bound by the latency
+// of its key tiles: some 768 workgroups, of three tiles at least.  One of many rows computes, and its parts cost their O in fp32
+// twice: some 384 workgroups of four wavefronts, of six tiles at least, and nothing below 16.
+// Forward, us, in one part -> as here (best of 1 to 32), lengths log-normal with a spread of .4:
+//   rows to 32: 32 samples of one token, some 1700 keys, 32/8 heads of 128: 72.8 -> 44.9 (44.9); 4 of 64: 43.0 -> 20.7 (20.6)
+//               1 token, 19278 keys, 32/8 heads: 269 -> 26.8 (26.8); 8 tokens, 24 heads: 41.6 -> 33.2 (31.8); 16 of 192: 59.5 -> 40.0 (34.4)
+//   more:       64 queries, 4000 keys: 59.0 -> 21.6 (21.6), 64/8: 50.6 -> 26 (24.5); 4 samples: 50.4 -> 29.8 (29.7)
+//               256 queries, 8000 keys, 32/8 heads: 131 -> 48.4 (45.3); 1308, 16859 keys, 8/1: 269 -> 113 (98.7)
+//               517, 12494 keys, 64/8: 260 in one part (231 in three); 16 samples of 100 queries, 300 keys: 12 to 41 in one part,
+//               14 to 85 in two
 inline int cross_fwd_parts(const hbp_cross_desc& d) {
   if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return 1;
-  const int l = cross_fold_log2(d);
-  const int64_t full = (((int64_t)d.total_queries << l) + kCrossRows - 1) / kCrossRows, some = d.n_samples < d.total_queries ? d.n_samples : d.total_queries;
-  const int64_t items = (full > some ? full : some) * (d.n_q_heads >> l), keys = d.total_keys / d.n_samples;
-  int64_t parts = 2048 / items;
-  if (parts > keys / 128) parts = keys / 128;
-  return (int)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+  const CrossTiles t = cross_tiles(d);
+  int64_t parts, most;
+  if (t.rows <= 32) {
+    parts = 768 / t.items;
+    most = t.key_tiles / 3 < 32 ? t.key_tiles / 3 : 32;
+  } else {
+    parts = 384 / (t.items * ((t.rows + 127) / 128));
+    most = t.key_tiles < 16 ? 1 : t.key_tiles / 6 < 16 ? t.key_tiles / 6 : 16;
+  }
+  if (parts > most) parts = most;
+  return (int)(parts < 1 ? 1 : parts);
 }
 struct CrossFwdLayout {
   size_t o_off, ml_off, total;
@@ -66,9 +95,39 @@ inline CrossFwdLayout cross_fwd_layout(const hbp_cross_desc& d) {
   return l;
 }
 
+// The same for dQ, beside dK/dV in one launch.  In products of 64-column blocks: an item of dQ takes 3 x 256 rows x its keys, all
+// of dQ that times its items, all of dK/dV 4 x rows x keys.  An item that is longer than a compute unit's share of the two is cut.
+// Backward, us, in one part -> as here: 118 queries, 7467 keys, 32/8 heads of 128: 172 -> 69; 74, 5994, 6/2 of 64: 73 -> 22.5; 34,
+// 5300, 8/1: 109 -> 24; 112, 5400, 12/3: 117 -> 31; 52, 4222, 24: 103 -> 50.  (By the forward's rule 16 samples of 450 queries and
+// 800 keys, 8/1 heads, went from 132 to 167.)
+inline int cross_dq_parts(const hbp_cross_desc& d) {
+  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return 1;
+  const CrossTiles t = cross_tiles(d);
+  int64_t parts = 256 * 3 * kCrossRows / (t.items * 3 * kCrossRows + (int64_t)d.total_queries * d.n_q_heads * 4);
+  if (parts > t.key_tiles / 2) parts = t.key_tiles / 2;
+  return (int)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+}
+
+// Workgroups that share the rows of a tile where parts are added up: some 1024 in all, and no more than a tile has work for.
+inline int cross_join_shares(int groups, int tiles) {
+  const int64_t n = 1024 / ((int64_t)groups * tiles);
+  return n < 4 ? 4 : n > 32 ? 32 : (int)n;
+}
+
+// Whether the items of dQ are longer than those of dK/dV in the mean: a step over 64 keys costs one of dQ's 256 rows three
+// products, a step over 64 rows one of dK/dV's 128 keys four.
+inline bool cross_dq_first(int64_t queries, int64_t keys, int group, int parts, int dq_parts) {
+  return keys * 3 * 256 / dq_parts > queries * group * 4 * 128 / parts;
+}
+
+// dK/dV and dQ in one launch, a workgroup of eight wavefronts an item, as long as the items' numbers stay exact in the kernel's
+// quotients (head sizes 64 and 128; at 192 the two have a launch each).  Against two launches, 56 packs of 550 to 19600 tokens a
+// side, 1/1 to 64/8 heads: 1.3 to 1.6 where the launches have few rounds, 1.0 to 1.1 in large packs, .99 at worst.
+inline bool cross_one_launch(int64_t n_dkdv, int64_t n_dq) { return n_dkdv > 0 && n_dq > 0 && n_dkdv + n_dq < (1 << 22); }
+
 struct CrossBwdLayout {
-  size_t d_off, lse2_off, dk_part_off, dv_part_off, total;
-  int parts;
+  size_t d_off, lse2_off, dk_part_off, dv_part_off, dq_part_off, total;
+  int parts, dq_parts;
 };
 inline CrossBwdLayout cross_bwd_layout(const hbp_cross_desc& d) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -79,7 +138,9 @@ inline CrossBwdLayout cross_bwd_layout(const hbp_cross_desc& d) {
   l.lse2_off = rows;
   l.dk_part_off = 2 * rows;
   l.dv_part_off = l.dk_part_off + up(sums * d.d_qk);
-  l.total = l.dv_part_off + up(sums * d.d_v);
+  l.dq_parts = cross_dq_parts(d);
+  l.dq_part_off = l.dv_part_off + up(sums * d.d_v);
+  l.total = l.dq_part_off + (l.dq_parts > 1 ? up((size_t)l.dq_parts * d.n_q_heads * d.total_queries * d.d_qk * 4) : 0);
   return l;
 }
 

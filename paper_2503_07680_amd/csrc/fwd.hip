@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "cross_rules.hpp"
 
 namespace hbp {
 
@@ -395,12 +396,12 @@ __device__ __forceinline__ void fwd_items() {
     const int halves = HP * TP == 1 ? p.halves : 0, half = __builtin_popcount(tile_idx) & halves;
     hbp_tile tl;
     int s0, s1;
-    bool ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.n_samples, lane, tl, s0, s1);
     int ks0 = 0, ks1 = 0;
+    bool ok;
+    if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.cu_kv, p.n_samples, lane, tl, s0, s1, ks0, ks1);
+    else ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.n_samples, lane, tl, s0, s1);
     if constexpr (CROSS) {
       if (ok) {
-        ks0 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample]);
-        ks1 = __builtin_amdgcn_readfirstlane(p.cu_kv[tl.sample + 1]);
         ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= (BM << halves) >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
              BM * half < (tl.row_end - tl.row_begin) << p.fold_log2;
@@ -690,8 +691,7 @@ __global__ __launch_bounds__(kThreads * TP, 2 / TP) void cross_forward_kernel(co
 
 // O and LSE of a tile's rows from their parts: with m the largest of the references m_i, O = sum 2^(m_i - m) O_i / l and
 // LSE = (m + log2 l) ln 2, l = sum 2^(m_i - m) l_i.  DV / 4 lanes a row; bound by reading the parts once.  Grid: folded groups,
-// kJoinShares workgroups, tiles.
-constexpr int kJoinShares = 4;
+// shares of the rows, tiles.
 template <int DV>
 __global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p) {
   constexpr int LPR = DV / 4;
@@ -704,7 +704,7 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p)
     return;
   const int n_rows = (tl.row_end - tl.row_begin) << p.fold_log2, x = threadIdx.x % LPR;
   const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
-  for (int f = blockIdx.y * (kThreads / LPR) + threadIdx.x / LPR; f < n_rows; f += kJoinShares * (kThreads / LPR)) {
+  for (int f = blockIdx.y * (kThreads / LPR) + threadIdx.x / LPR; f < n_rows; f += gridDim.y * (kThreads / LPR)) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     for (int at = 0; at < p.parts; at += 4) {  // four parts' loads under way
@@ -815,7 +815,7 @@ static int launch_cross_fwd_t(FwdParams p, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
     if (p.parts > 1) {
-      hipLaunchKernelGGL((cross_join_kernel<DV>), dim3((unsigned)(p.Hkv * p.g), kJoinShares, (unsigned)(part.n_tiles >> p.halves)), dim3(kThreads), 0, s, part);
+      hipLaunchKernelGGL((cross_join_kernel<DV>), dim3((unsigned)(p.Hkv * p.g), cross_join_shares(p.Hkv * p.g, part.n_tiles >> p.halves), (unsigned)(part.n_tiles >> p.halves)), dim3(kThreads), 0, s, part);
       e = hipGetLastError();
       if (e != hipSuccess) return (int)e;
     }
