@@ -5,10 +5,13 @@
 //
 // Both move bytes and compute next to nothing.  The gradient works on the tokens sorted by id, equal ids in the order of
 // their positions, so that every row of dW is summed in one fixed order, in 32 bits, and written once, without atomics:
-// (1) a stable radix sort of (id, position), nine bits of the id a pass; (2) the sorted positions are cut into chunks of a
-// fixed number, whatever the ids, so that a frequent id costs no workgroup more than the others: a run of equal ids inside a
-// chunk is summed and written, of one that goes beyond it the chunk's part is kept; (3) the parts of such runs are added up
-// in the chunks' order.  A fresh dW is zeroed beside the sort, which leaves the chip idle otherwise.
+// (1) the stable sort of (id, position); (2) the sorted positions are cut into chunks of a fixed number, whatever the ids, so
+// that a frequent id costs no workgroup more than the others: a run of equal ids inside a chunk is summed and written, of one
+// that goes beyond it the chunk's part is kept; (3) the parts of such runs are added up in the chunks' order.
+//
+// The sort is one launch (embed_group_kernel): a workgroup owns a range of up to 1024 ids, reads all tokens twice (32 KB to 1 MB,
+// from its die's L2), counts those below its range, which is where its part of the order begins, and places its own.  It
+// also zeroes those rows of a fresh dW that have no token.  Very many tokens or ids take a radix sort of nine bits a pass instead.
 #include "rows.hpp"
 
 namespace hbp {
@@ -18,13 +21,20 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kOneTile = 16384;              // tokens that one workgroup sorts by itself
+constexpr int kGroupTile = 16384, kGroupBins = 1024;  // tokens that are placed at a time, ids of a workgroup (embed_group_kernel)
 constexpr int kTileRounds = 4, kTile = kTileRounds * kSortThreads;  // of each workgroup where there are more
 constexpr int kSmallChunks = 16384;          // up to so many tokens: chunks of 16, else of 32
 constexpr uint32_t kNoKey = 0xffffffffu;
 
 int log2_threads_per_row(int n_vec) {  // 64 to 256: a wavefront is always on one row
   return n_vec > 128 ? 8 : n_vec > 64 ? 7 : 6;
+}
+int waves_per_row(int n_vec) { return (n_vec + 63) / 64; }
+// Ids of a workgroup of the one-launch sort; 0: that reads too much (a quarter of a million tokens for each of 256 workgroups
+// or more), the radix sort is taken.
+int group_bins(int32_t T, int32_t V) {
+  const int bins = V <= 256 * kGroupBins ? (V + 255) / 256 : kGroupBins;
+  return (int64_t)T * ((V + (int64_t)bins - 1) / bins) <= ((int64_t)1 << 26) ? bins : 0;
 }
 int n_vectors(int dim) { return dim >= 8 ? (dim + 7) / 8 : dim; }
 int key_bits(int32_t V) { return 32 - __builtin_clz((uint32_t)V); }  // ids 0 .. V - 1, and V for "no token"
@@ -160,81 +170,163 @@ struct Fill {
   int64_t stride_bytes, row_bytes;
   int32_t V, part, parts, blocks;  // blocks: 0 for none
 };
+__device__ __forceinline__ void zero_row(const Fill& f, int64_t r, int lane) {
+  char* row = f.table + r * f.stride_bytes;
+  int64_t b = lane * 16;
+  for (; b + 16 <= f.row_bytes; b += 1024) __builtin_nontemporal_store(u32x4_any{0, 0, 0, 0}, (u32x4_any*)(row + b));
+  // at most one piece of the row's end is left, to one lane; rows are whole elements of 2 or 4 bytes
+  if (b < f.row_bytes)
+    for (; b < f.row_bytes; b += 2) *(uint16_t*)(row + b) = 0;
+}
 __device__ __forceinline__ void fill_rows(const Fill& f, int block) {
   const int lane = threadIdx.x & 63;
   const int64_t waves = (int64_t)f.blocks * kSortWaves, wave = (int64_t)block * kSortWaves + (threadIdx.x >> 6);
   const int64_t from = (int64_t)f.V * f.part / f.parts, to = (int64_t)f.V * (f.part + 1) / f.parts;
-  for (int64_t r = from + wave; r < to; r += waves) {
-    char* row = f.table + r * f.stride_bytes;
-    int64_t b = lane * 16;
-    for (; b + 16 <= f.row_bytes; b += 1024) __builtin_nontemporal_store(u32x4_any{0, 0, 0, 0}, (u32x4_any*)(row + b));
-    // at most one piece of the row's end is left, to one lane; rows are whole elements of 2 or 4 bytes
-    if (b < f.row_bytes)
-      for (; b < f.row_bytes; b += 2) *(uint16_t*)(row + b) = 0;
+  for (int64_t r = from + wave; r < to; r += waves) zero_row(f, r, lane);
+}
+
+// The one-launch sort: workgroup w owns the ids [w bins, (w + 1) bins).  First all tokens are read for the numbers of each of its
+// ids and of all smaller ones; then again, kGroupTile at a time, for their places: the tile's tokens of its ids are listed in
+// LDS in order, a wavefront ranks 64 listed ones among those of the same id by ballots over the bits, and the counts of the
+// wavefronts in front, of the tiles in front and of the smaller ids make up the rest of a place.
+// 8192 tokens, 128256 ids: 26.8 us with one workgroup sorting 9 bits at a time in LDS.
+struct GroupLds {
+  uint16_t counts[kGroupBins * kSortWaves];  // of the tile, [id][wavefront]
+  uint16_t id[kGroupTile], pos[kGroupTile], rank[kGroupTile];
+  uint32_t place[kGroupBins];                // counts, then the next place, of each id
+  uint32_t sums[kSortWaves], below[kSortWaves];
+  uint64_t has[kSortWaves];                  // ids with a token, a bit each
+};
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ i32x4_any load_tokens(const int32_t* tokens, int T, int i) {  // -1 behind the last
+  if (i + 4 <= T) return *(const i32x4_any*)(tokens + i);
+  i32x4_any t;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j] = i + j < T ? tokens[i + j] : -1;
+  return t;
+}
+__global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t* tokens, int T, int V, int bins, uint32_t* keys,
+                                                                   uint32_t* order, Fill fill) {
+  extern __shared__ __attribute__((aligned(16))) char group_lds[];
+  GroupLds& l = *(GroupLds*)group_lds;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int lo = (int)((int64_t)blockIdx.x * bins), mine = min(bins, V - lo);
+  const uint64_t in_front = ((uint64_t)1 << lane) - 1;
+  auto of_mine = [&](int t) { return (uint32_t)(t - lo) < (uint32_t)mine; };  // tokens that are none are below 0 or from V on
+  l.place[tid] = 0;
+  __syncthreads();
+  uint32_t below = 0;  // of this wavefront
+  for (int i0 = wave * 256; i0 < T; i0 += kSortWaves * 256) {
+    const i32x4_any t = load_tokens(tokens, T, i0 + lane * 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      below += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)t[j] < (uint32_t)lo));
+      if (of_mine(t[j])) atomicAdd(&l.place[t[j] - lo], 1u);  // whole numbers: the order does not matter
+    }
+  }
+  if (lane == 0) l.below[wave] = below;
+  __syncthreads();
+  const uint32_t own = l.place[tid];
+  const uint64_t has = __builtin_amdgcn_ballot_w64(own != 0);
+  if (lane == 0) l.has[wave] = has;
+  uint32_t base = 0;
+  for (int w = 0; w < kSortWaves; ++w) base += l.below[w];
+  const uint32_t place = base + before_me(own, l.sums);
+  __syncthreads();
+  l.place[tid] = place;
+  const uint32_t end = __builtin_amdgcn_readfirstlane(base + l.sums[0] + l.sums[1] + l.sums[2] + l.sums[3] + l.sums[4] + l.sums[5] + l.sums[6] + l.sums[7] +
+                                                      l.sums[8] + l.sums[9] + l.sums[10] + l.sums[11] + l.sums[12] + l.sums[13] + l.sums[14] + l.sums[15]);
+  for (int t0 = 0; t0 < T; t0 += kGroupTile) {
+    // the wavefront's 1024 tokens of the tile
+    i32x4_any t[4];
+    uint32_t listed = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      t[k] = load_tokens(tokens, T, t0 + wave * 1024 + k * 256 + lane * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) listed += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(of_mine(t[k][j])));
+    }
+    __syncthreads();  // the tile before is placed
+    for (int i = tid; i < kGroupBins * kSortWaves / 8; i += kSortThreads) ((u32x4_any*)l.counts)[i] = u32x4_any{0, 0, 0, 0};
+    if (lane == 0) l.sums[wave] = listed;
+    __syncthreads();
+    uint32_t at = 0, n = 0;
+    for (int w = 0; w < kSortWaves; ++w) {
+      if (w < wave) at += l.sums[w];
+      n += l.sums[w];
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    if (n == 0) continue;
+    if (listed) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint64_t b[4];
+        uint32_t to = at;  // of this lane's first: the lanes in front, four tokens each
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          b[j] = __builtin_amdgcn_ballot_w64(of_mine(t[k][j]));
+          to += (uint32_t)__popcll(b[j] & in_front);
+          at += (uint32_t)__popcll(b[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (of_mine(t[k][j])) {
+            l.id[to] = (uint16_t)(t[k][j] - lo);
+            l.pos[to] = (uint16_t)(wave * 1024 + k * 256 + lane * 4 + j);
+            ++to;
+          }
+      }
+    }
+    __syncthreads();
+    const int rounds = (int)((n + kSortThreads - 1) / kSortThreads), first = wave * rounds * 64 + lane;
+    volatile uint16_t* const counts = l.counts;
+    for (int e = 0; e < rounds; ++e) {
+      const uint32_t i = first + e * 64;
+      const bool is = i < n;
+      const uint32_t d = is ? l.id[i] : 0;
+      uint64_t same = __builtin_amdgcn_ballot_w64(is);
+#pragma unroll
+      for (int b = 0; b < 10; ++b) {
+        const bool one = (d >> b) & 1;
+        const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
+        same &= one ? ones : ~ones;
+      }
+      if (is) {  // LDS operations of a wavefront are in order: all read the count before the first of each id raises it
+        const uint32_t before = counts[d * kSortWaves + wave], r = (uint32_t)__popcll(same & in_front);
+        __builtin_amdgcn_wave_barrier();
+        if (r == 0) counts[d * kSortWaves + wave] = (uint16_t)(before + (uint32_t)__popcll(same));
+        __builtin_amdgcn_wave_barrier();
+        l.rank[i] = (uint16_t)(before + r);
+      }
+    }
+    __syncthreads();
+    for (int e = 0; e < rounds; ++e) {
+      const uint32_t i = first + e * 64;
+      if (i >= n) break;
+      const uint32_t d = l.id[i];
+      uint32_t to = l.place[d] + l.rank[i];
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) to += w < wave ? l.counts[d * kSortWaves + w] : 0;
+      keys[to] = (uint32_t)lo + d;
+      order[to] = (uint32_t)t0 + l.pos[i];
+    }
+    if (t0 + kGroupTile < T) {
+      __syncthreads();
+      for (int e = 0; e < rounds; ++e) {
+        const uint32_t i = first + e * 64;
+        if (i < n) atomicAdd(&l.place[l.id[i]], 1u);
+      }
+    }
+  }
+  if ((int)blockIdx.x == (int)gridDim.x - 1)  // behind the last token: none
+    for (int64_t i = (int64_t)end + tid; i < T; i += kSortThreads) keys[i] = (uint32_t)V;
+  if (fill.blocks) {
+    for (int r = wave; r < mine; r += kSortWaves)
+      if (!(l.has[r >> 6] >> (r & 63) & 1)) zero_row(fill, lo + r, lane);
   }
 }
 
-// T <= kOneTile: the first workgroup sorts in LDS, the others zero dW.
-template <int ROUNDS>
-__global__ __launch_bounds__(kSortThreads) void embed_sort_one_kernel(const int32_t* tokens, int T, int V, int bits, uint32_t* keys,
-                                                                      uint32_t* order, Fill fill) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-  if (blockIdx.x > 0) {
-    fill_rows(fill, blockIdx.x - 1);
-    return;
-  }
-  constexpr int N = ROUNDS * kSortThreads;
-  uint32_t* const counts = lds;
-  uint32_t* const sums = lds + kDigits * kSortWaves;
-  uint32_t* const key_lds = sums + kSortWaves;
-  uint16_t* const pos_lds = (uint16_t*)(key_lds + N);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, rounds = (T + kSortThreads - 1) / kSortThreads;
-  uint32_t key[ROUNDS], rank[ROUNDS];
-  uint32_t pos[ROUNDS];
-#pragma unroll
-  for (int e = 0; e < ROUNDS; ++e) {
-    const int i = (wave * rounds + e) * 64 + lane;
-    const bool is = e < rounds && i < T;
-    key[e] = is ? key_of(tokens[is ? i : 0], V) : kNoKey;
-    pos[e] = i;
-  }
-  for (int shift = 0; shift < bits; shift += kDigitBits) {
-    clear_counts(counts);
-    wave_ranks<ROUNDS>(key, rank, rounds, shift, (LdsCounts)counts);
-    __syncthreads();
-    scan_counts(counts, sums);
-    const bool last = shift + kDigitBits >= bits;
-#pragma unroll
-    for (int e = 0; e < ROUNDS; ++e) {
-      if (e >= rounds || key[e] == kNoKey) continue;
-      const uint32_t to = counts[((key[e] >> shift) & (kDigits - 1)) * kSortWaves + wave] + rank[e];
-      key_lds[to] = key[e];
-      pos_lds[to] = (uint16_t)pos[e];
-    }
-    __syncthreads();
-    if (last) {
-      for (int i = threadIdx.x; i < T; i += kSortThreads) {
-        keys[i] = key_lds[i];
-        order[i] = pos_lds[i];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < ROUNDS; ++e) {
-        const int i = (wave * rounds + e) * 64 + lane;
-        const bool is = e < rounds && i < T;
-        key[e] = is ? key_lds[i] : kNoKey;
-        pos[e] = is ? pos_lds[i] : 0;
-      }
-    }
-    // clear_counts has a barrier in front of the next pass's scatter
-  }
-}
-template <int ROUNDS>
-constexpr int sort_one_lds() {
-  return (kDigits * kSortWaves + kSortWaves) * 4 + ROUNDS * kSortThreads * 6;
-}
-
-// More tokens: a workgroup a tile.  counts[tile][digit] of one pass; first pass: the keys are the tokens.
+// The radix sort: a workgroup a tile.  counts[tile][digit] of one pass; first pass: the keys are the tokens.
 __global__ __launch_bounds__(kSortThreads) void embed_count_kernel(const int32_t* tokens, const uint32_t* keys, int T, int V, int shift,
                                                                    int tiles, uint32_t* counts, Fill fill) {
   __shared__ uint32_t c[kDigits];
@@ -339,10 +431,10 @@ struct Sorted {
 
 template <int ROW, int TABLE, int VEC, int U>
 __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, Sorted s, const typename RowType<ROW>::T* d_out,
-                                                                typename RowType<TABLE>::T* d_table, bool accumulate, int log2_tpr) {
-  const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> log2_tpr);
-  const int c = blockIdx.x * (kRowThreads >> log2_tpr) + sub;
-  const int v = (blockIdx.y << log2_tpr) + (threadIdx.x & ((1 << log2_tpr) - 1));
+                                                                typename RowType<TABLE>::T* d_table, bool accumulate, int wpr) {
+  // a wavefront takes 64 vectors of a chunk's rows
+  const int64_t w = (int64_t)blockIdx.x * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int c = (int)(w / wpr), v = (int)(w - (int64_t)c * wpr) * 64 + (threadIdx.x & 63);
   const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
   if (c >= s.n_chunks || v >= n_vec) return;
   const Span at = span_of<VEC>(v, p.dim);
@@ -382,9 +474,9 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, S
 
 // The run that begins in chunk c and goes beyond it: its parts, in the chunks' order.
 template <int TABLE, int VEC>
-__global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, Sorted s, typename RowType<TABLE>::T* d_table, bool accumulate, int log2_tpr) {
-  const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> log2_tpr);
-  const int c = blockIdx.x * (kRowThreads >> log2_tpr) + sub;
+__global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, Sorted s, typename RowType<TABLE>::T* d_table, bool accumulate, int wpr) {
+  const int64_t w = (int64_t)blockIdx.x * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int c = (int)(w / wpr);
   if (c + 1 >= s.n_chunks) return;  // nothing goes beyond the last one
   const int first = c * s.chunk, next = first + s.chunk;
   const uint32_t k = s.keys[next - 1];
@@ -397,7 +489,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, 
     n += __popcll(in);
     if (~in) break;
   }
-  const int v = (blockIdx.y << log2_tpr) + (threadIdx.x & ((1 << log2_tpr) - 1));
+  const int v = (int)(w - (int64_t)c * wpr) * 64 + (threadIdx.x & 63);
   const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
   if (v >= n_vec) return;
   const Span at = span_of<VEC>(v, p.dim);
@@ -428,26 +520,27 @@ void lookup(const EmbedParams& p, const void* table, void* out, hipStream_t s) {
 
 template <int ROW, int TABLE, int VEC>
 int sums(const EmbedParams& p, const Sorted& srt, const void* d_out, void* d_table, bool accumulate, hipStream_t s) {
-  const int n_vec = n_vectors(p.dim), log2_tpr = log2_threads_per_row(n_vec), per_group = kRowThreads >> log2_tpr;
-  const dim3 grid((unsigned)((srt.n_chunks + per_group - 1) / per_group), (unsigned)((n_vec + (1 << log2_tpr) - 1) >> log2_tpr));
+  const int wpr = waves_per_row(n_vectors(p.dim)), per_group = kRowThreads / 64;
+  const int64_t groups = ((int64_t)srt.n_chunks * wpr + per_group - 1) / per_group;
+  if (groups > 0x7fffffff) return (int)hipErrorInvalidValue;
+  const dim3 grid((unsigned)groups);
   auto* w = (typename RowType<TABLE>::T*)d_table;
-  hipLaunchKernelGGL((embed_sum_kernel<ROW, TABLE, VEC, 8>), grid, dim3(kRowThreads), 0, s, p, srt, (const typename RowType<ROW>::T*)d_out, w, accumulate, log2_tpr);
+  hipLaunchKernelGGL((embed_sum_kernel<ROW, TABLE, VEC, 8>), grid, dim3(kRowThreads), 0, s, p, srt, (const typename RowType<ROW>::T*)d_out, w, accumulate, wpr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || srt.n_chunks < 2) return (int)e;
-  hipLaunchKernelGGL((embed_join_kernel<TABLE, VEC>), grid, dim3(kRowThreads), 0, s, p, srt, w, accumulate, log2_tpr);
+  hipLaunchKernelGGL((embed_join_kernel<TABLE, VEC>), grid, dim3(kRowThreads), 0, s, p, srt, w, accumulate, wpr);
   return (int)hipGetLastError();
 }
 
-template <int ROUNDS>
-int sort_one(const EmbedParams& p, int bits, uint32_t* keys, uint32_t* order, const Fill& fill, hipStream_t s) {
-  constexpr int lds = sort_one_lds<ROUNDS>();
+int group(const EmbedParams& p, int bins, uint32_t* keys, uint32_t* order, const Fill& fill, hipStream_t s) {
   static bool attr_set = false;
   if (!attr_set) {
-    const hipError_t e = hipFuncSetAttribute((const void*)embed_sort_one_kernel<ROUNDS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute((const void*)embed_group_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GroupLds));
     if (e != hipSuccess) return (int)e;
     attr_set = true;
   }
-  hipLaunchKernelGGL((embed_sort_one_kernel<ROUNDS>), dim3(1 + fill.blocks), dim3(kSortThreads), lds, s, p.tokens, p.T, p.V, bits, keys, order, fill);
+  hipLaunchKernelGGL(embed_group_kernel, dim3((unsigned)((p.V + (int64_t)bins - 1) / bins)), dim3(kSortThreads), sizeof(GroupLds), s, p.tokens, p.T, p.V, bins,
+                     keys, order, fill);
   return (int)hipGetLastError();
 }
 
@@ -471,7 +564,7 @@ EmbedBwdLayout embed_bwd_layout(int32_t T, int32_t V, int32_t dim) {
   const size_t ints = up((size_t)T * 4), tiles = (size_t)(T / kTile + 1);
   l.keys_off[0] = 0;
   l.order_off[0] = ints;
-  const bool one = T <= kOneTile;  // sorted where it ends
+  const bool one = group_bins(T, V) != 0;  // sorted where it ends
   l.keys_off[1] = one ? 0 : 2 * ints;
   l.order_off[1] = one ? ints : 3 * ints;
   l.hist_off = one ? 2 * ints : 4 * ints;
@@ -479,7 +572,6 @@ EmbedBwdLayout embed_bwd_layout(int32_t T, int32_t V, int32_t dim) {
   // fewer tokens never need more: a workspace for the longest pack serves all
   const size_t parts = (size_t)(T <= kSmallChunks ? l.n_chunks : l.n_chunks > kSmallChunks / 16 ? l.n_chunks : kSmallChunks / 16);
   l.total = l.part_off + up(parts * 2 * (size_t)dim * 4);
-  (void)V;
   return l;
 }
 
@@ -493,10 +585,10 @@ int launch_embed_bwd(const EmbedParams& p, int table_type, int row_type, const v
   // workgroups of 16 wavefronts, a row a wavefront at a time
   const int fill_blocks = accumulate ? 0 : (int)((p.V + kSortWaves - 1) / kSortWaves < 2048 ? (p.V + kSortWaves - 1) / kSortWaves : 2048);
   int at = 0;
-  if (p.T <= kOneTile) {
-    fill.blocks = fill_blocks;
-    if (p.T == 0 && accumulate) return 0;
-    const int e = p.T <= 4096 ? sort_one<4>(p, bits, keys[0], order[0], fill, s) : sort_one<16>(p, bits, keys[0], order[0], fill, s);
+  if (p.T == 0 && accumulate) return 0;
+  if (const int bins = group_bins(p.T, p.V)) {
+    fill.blocks = accumulate ? 0 : 1;
+    const int e = group(p, bins, keys[0], order[0], fill, s);
     if (e || p.T == 0) return e;
   } else {
     const int tiles = (p.T + kTile - 1) / kTile, passes = (bits + kDigitBits - 1) / kDigitBits;

@@ -54,6 +54,9 @@ CASES = [  # tokens, vocab, dim, ids
     (16384, 513, 40, "skewed"), (16385, 32000, 24, "skewed"), (20000, 600000, 8, "any"), (40001, 5000, 15, "skewed"),
     (3000, 200, 1025, "same"), (33000, 40, 65, "same"), (700, 128, 2056, "none"), (17000, 64, 12, "none"),
     (16, 100, 5120, "same"), (17, 100, 5124, "same"),
+    # several tiles of the one-launch sort, ranges of 1024 ids and a short last one; then the radix sort: many tokens, many ids
+    (49152, 262144, 8, "any"), (70000, 262145, 9, "skewed"), (500001, 300, 8, "skewed"), (8001, 9000000, 1, "any"),
+    (270000, 70000, 2, "any"),
 ]
 
 
