@@ -546,6 +546,14 @@ hbp_status hbp_grad_clip(const void* const* tensors, void* const* outs_or_null, 
                          int32_t n_tensors, const double* sumsq, float max_norm, float* norm_out_or_null, void* stream);
 
 /*
+ * hbp_grad_clip_norm — both in one call, for gradients that are whole on this GPU: *sumsq_out as hbp_grad_sumsq would write it
+ * and the clipping by it, the same bits as with the two calls.  Same arguments and errors.
+ */
+hbp_status hbp_grad_clip_norm(const void* const* tensors, void* const* outs_or_null, const int64_t* sizes, const int32_t* types,
+                              int32_t n_tensors, float max_norm, double* sumsq_out, float* norm_out_or_null, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
  * hbp_mfma_probe — measurement aid: the second denominator of the roofline.  Launches, on `stream`,
  * one kernel in which every SIMD of `n_cu` compute units (two wavefronts each) issues nothing but
  * independent 32x32x16 bf16 MFMAs on register-resident data: `mfma_per_wave` of them per wavefront

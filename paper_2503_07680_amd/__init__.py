@@ -10,7 +10,7 @@ from .binding import (HbpError, AttnDesc, load_library, library_path, hbp_status
                       HBP_TILES_QUERY, HBP_TILES_KEY, PROFILE_DTYPE, EXPORTED_SYMBOLS,
                       CrossDesc, hbp_cross_tile_rows, hbp_cross_plan, hbp_cross_workspace_bytes, hbp_cross_attn_fwd, hbp_cross_attn_bwd,
                       EmbedDesc, hbp_embed_fwd, hbp_embed_bwd_workspace_bytes, hbp_embed_bwd,
-                      GradList, hbp_grad_workspace_bytes, hbp_grad_sumsq, hbp_grad_clip, HBP_BF16, HBP_F32)
+                      GradList, hbp_grad_workspace_bytes, hbp_grad_sumsq, hbp_grad_clip, hbp_grad_clip_norm, HBP_BF16, HBP_F32)
 
 __all__ = ["HbpError", "AttnDesc", "load_library", "library_path", "hbp_status_string",
            "hbp_pack_plan", "hbp_order_query_tiles", "hbp_tile_rows", "hbp_fwd_tile_rows", "hbp_workspace_bytes", "hbp_profile_capacity",
@@ -19,4 +19,4 @@ __all__ = ["HbpError", "AttnDesc", "load_library", "library_path", "hbp_status_s
            "HBP_TILES_QUERY", "HBP_TILES_KEY", "PROFILE_DTYPE", "EXPORTED_SYMBOLS",
            "CrossDesc", "hbp_cross_tile_rows", "hbp_cross_plan", "hbp_cross_workspace_bytes", "hbp_cross_attn_fwd", "hbp_cross_attn_bwd",
            "EmbedDesc", "hbp_embed_fwd", "hbp_embed_bwd_workspace_bytes", "hbp_embed_bwd",
-           "GradList", "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip", "HBP_BF16", "HBP_F32"]
+           "GradList", "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip", "hbp_grad_clip_norm", "HBP_BF16", "HBP_F32"]

@@ -20,7 +20,7 @@ EXPORTED_SYMBOLS = ["hbp_status_string", "hbp_pack_plan", "hbp_order_query_tiles
                     "hbp_packed_ce_workspace_bytes", "hbp_packed_ce", "hbp_auto_select",
                     "hbp_cross_tile_rows", "hbp_cross_plan", "hbp_cross_workspace_bytes", "hbp_cross_attn_fwd",
                     "hbp_cross_attn_bwd", "hbp_embed_fwd", "hbp_embed_bwd_workspace_bytes", "hbp_embed_bwd",
-                    "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip"]
+                    "hbp_grad_workspace_bytes", "hbp_grad_sumsq", "hbp_grad_clip", "hbp_grad_clip_norm"]
 
 # numpy views of hbp_pack / hbp_batch
 PACK_DTYPE = np.dtype([("level", "<i4"), ("first_item", "<i4"), ("n_items", "<i4"), ("n_tokens", "<i4"),
@@ -172,6 +172,8 @@ def load_library():
     lib.hbp_grad_sumsq.argtypes = [vp, vp, vp, i32, i32, vp, vp, ctypes.c_size_t, vp]
     lib.hbp_grad_clip.restype = i32
     lib.hbp_grad_clip.argtypes = [vp, vp, vp, vp, i32, vp, ctypes.c_float, vp, vp]
+    lib.hbp_grad_clip_norm.restype = i32
+    lib.hbp_grad_clip_norm.argtypes = [vp, vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     _lib = lib
     return lib
 
@@ -516,6 +518,16 @@ def hbp_grad_clip(grads: GradList, sumsq, max_norm: float, norm_out=None, stream
                                       _ptr(norm_out), stream)
     if st != 0:
         raise HbpError(st, "hbp_grad_clip")
+
+
+def hbp_grad_clip_norm(grads: GradList, max_norm: float, sumsq, norm_out, workspace, stream: Optional[int] = None) -> None:
+    """Both of the above in one call."""
+    tensors, sizes, types, outs = grads.args
+    st = load_library().hbp_grad_clip_norm(tensors, outs, sizes, types, grads.n, float(max_norm), _ptr(sumsq),
+                                           _ptr(norm_out), _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                                           stream)
+    if st != 0:
+        raise HbpError(st, "hbp_grad_clip_norm")
 
 
 def hbp_mfma_probe(n_cu: int, mfma_per_wave: int, sink, stream=None) -> None:

@@ -78,19 +78,30 @@ EmbedBwdLayout embed_bwd_layout(int32_t T, int32_t V, int32_t dim);
 int launch_embed_bwd(const EmbedParams& p, int table_type, int row_type, const void* d_out, void* d_table, bool accumulate,
                      char* ws, hipStream_t s);
 
-// As many gradients as one launch's arguments hold.
-constexpr int kGradBatch = 120, kGradMaxGroups = 2048;
-constexpr int64_t kGradChunk = 16384;  // elements that a workgroup takes at a time
-struct GradBatch {
-  const void* in[kGradBatch];
-  void* out[kGradBatch];
-  int64_t size[kGradBatch];
-  uint32_t first_chunk[kGradBatch + 1];
-  uint8_t type[kGradBatch];
-  int32_t n;
+// A list of gradients as a launch's arguments: up to N tensors (a short list has short arguments: 3.5 KB of them cost a launch
+// 1.6 us on the host).  Chunks of 1 << chunk_log2 elements are dealt to the workgroups in turn.
+constexpr int kGradBatch = 120, kGradFew = 24, kGradMaxGroups = 2048;
+constexpr int kGradChunkLog2 = 14, kGradSmallChunkLog2 = 12;
+template <int N>
+struct GradBatchOf {
+  const void* in[N];
+  void* out[N];
+  int64_t size[N];
+  uint32_t first_chunk[N + 1];
+  uint8_t type[N];
+  int32_t n, chunk_log2;
 };
+typedef GradBatchOf<kGradBatch> GradBatch;
 int launch_grad_sumsq(const GradBatch& b, int groups, double* partial, hipStream_t s);
 int launch_grad_total(const double* partial, int n, double* sumsq, bool accumulate, hipStream_t s);
-int launch_grad_clip(const GradBatch& b, int groups, const double* sumsq, float max_norm, bool in_place, float* norm_out, hipStream_t s);
+// The sum of squares: sums[0] (n = 1), or the sum of n partial ones, which goes to sumsq_out then.
+struct GradNorm {
+  const double* sums;
+  int32_t n;
+  double* sumsq_out;
+  float max_norm;
+  float* norm_out;  // both outputs may be null
+};
+int launch_grad_clip(const GradBatch& b, int groups, const GradNorm& norm, bool in_place, hipStream_t s);
 
 }  // namespace hbp

@@ -315,7 +315,8 @@ class GradientClip:
 
     def clip(self, max_norm: float) -> torch.Tensor:
         """Norm of this object's tensors, and clipping to it; returns the norm (fp32, on the device)."""
-        return self.clip_with(self.sumsq(), max_norm)
+        _on(self.device, B.hbp_grad_clip_norm, self.list, max_norm, self.sumsq_buf, self.norm, self.ws)
+        return self.norm
 
 
 def bf16_tensor_to_f32_numpy(t: torch.Tensor) -> np.ndarray:

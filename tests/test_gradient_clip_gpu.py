@@ -59,6 +59,11 @@ def test_norm_and_clipping(sizes, offset):
         assert all(torch.equal(b, whole[t]) for t, b in buckets.items())      # the inputs stay
     for t, b in into.items():                                                   # and what lies beside the outputs
         assert torch.equal(b[:offset], beside[t][0]) and torch.equal(b[-1:], beside[t][1])
+    clip.clip(norm * 0.8)
+    one, n1, q1 = {t: b.clone() for t, b in into.items()}, clip.norm.clone(), clip.sumsq_buf.clone()
+    q2 = clip.sumsq().clone()                                                   # the two calls give the same bits
+    n2 = clip.clip_with(q2, norm * 0.8).clone()
+    assert torch.equal(q1, q2) and torch.equal(n1, n2) and all(torch.equal(b, one[t]) for t, b in into.items())
     place = GradientClip(grads)
     check(grads, before, norm, norm * 2, float(place.clip(norm * 2)))
     check(grads, before, norm, norm * 0.6, float(place.clip(norm * 0.6)))

@@ -70,12 +70,17 @@ def clip(g, max_norm=1.0, q=FAKE):
     return H.load_library().hbp_grad_clip(t, o, s, y, g.n, q, max_norm, None, None)
 
 
+def both(g, max_norm=1.0, q=FAKE, ws=FAKE, size=1 << 20):
+    t, s, y, o = g.args
+    return H.load_library().hbp_grad_clip_norm(t, o, s, y, g.n, max_norm, q, None, ws, size, None)
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(sizes=[100, -1, 100]), 1), (dict(types=[0, 1, 2]), 1), (dict(addresses=[FAKE, 0, 3 * FAKE]), 1),
     (dict(addresses=[FAKE, 2 * FAKE + 2, 3 * FAKE]), 1), (dict(sizes=[100, (1 << 40) + 1, 100]), 3),
 ])
 def test_gradient_lists(kw, status):
-    assert sumsq(grads(**kw)) == status and clip(grads(**kw)) == status
+    assert sumsq(grads(**kw)) == status and clip(grads(**kw)) == status and both(grads(**kw)) == status
 
 
 def test_gradient_calls():
@@ -83,7 +88,9 @@ def test_gradient_calls():
     assert sumsq(g, out=None) == 1 and sumsq(g, out=FAKE + 4) == 1 and sumsq(g, accumulate=2) == 1
     assert sumsq(g, ws=None) == 5 and sumsq(g, ws=FAKE + 8) == 5 and sumsq(g, size=8) == 5
     for bad in (-1.0, float("nan"), float("-inf")):
-        assert clip(g, max_norm=bad) == 1
+        assert clip(g, max_norm=bad) == 1 and both(g, max_norm=bad) == 1
+    assert both(g, q=None) == 1 and both(g, q=FAKE + 4) == 1
+    assert both(g, ws=None) == 5 and both(g, ws=FAKE + 8) == 5 and both(g, size=8) == 5
     assert clip(g, q=None) == 1 and clip(g, q=FAKE + 4) == 1
     assert lib.hbp_grad_sumsq(None, None, None, 2, 0, FAKE, FAKE, 1 << 20, None) == 1
     assert lib.hbp_grad_clip(None, None, None, None, -1, FAKE, 1.0, None, None) == 1
@@ -95,6 +102,7 @@ def test_gradient_calls():
 
 def test_overlapping_gradients_are_not_clipped():
     assert clip(grads(addresses=[FAKE, FAKE, 3 * FAKE])) == 1                            # the same tensor twice
+    assert both(grads(addresses=[FAKE, FAKE, 3 * FAKE])) == 1
     assert clip(grads(addresses=[FAKE, FAKE + 396, 3 * FAKE])) == 1                      # its last element
     far = [FAKE * (i + 10) for i in range(3)]
     assert clip(grads(outs=[far[0], far[0] + 4, far[2]])) == 1                           # two outputs
