@@ -42,6 +42,21 @@ __device__ __forceinline__ void for_chunks(const Batch& b, bool backwards, F f) 
   }
 }
 
+// Elements of a whole chunk in accesses of 16 bytes, a wavefront's beside each other: four or eight of them each.
+template <int TYPE>
+struct Quad {
+  static constexpr int N = 16 / sizeof(typename RowType<TYPE>::T);
+  typedef float Values __attribute__((ext_vector_type(N)));
+  static __device__ __forceinline__ Values widen(const u32x4_any& r) {
+    if constexpr (N == 8) return RowType<HBP_BF16>::widen(r);
+    else return __builtin_bit_cast(Values, r);
+  }
+  static __device__ __forceinline__ u32x4_any narrow(const Values& x) {
+    if constexpr (N == 8) return RowType<HBP_BF16>::narrow(x);
+    else return __builtin_bit_cast(u32x4_any, x);
+  }
+};
+
 template <int TYPE, int CHUNK>
 __device__ __forceinline__ double chunk_sumsq(const void* tensor, int64_t first, int n) {
   typedef RowType<TYPE> R;
@@ -55,13 +70,21 @@ __device__ __forceinline__ double chunk_sumsq(const void* tensor, int64_t first,
       q1 = fma((double)x[j + 1], (double)x[j + 1], q1);
     }
   };
-  constexpr int PASSES = CHUNK / (kThreads * 8);
+  typedef Quad<TYPE> Q;
+  constexpr int PASSES = CHUNK / (kThreads * Q::N);
   if (n == CHUNK) {
-    typename R::Raw x[PASSES];
+    u32x4_any raw[PASSES];
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u) x[u] = R::load_raw(p + 8 * (u * kThreads + (int)threadIdx.x));
+    for (int u = 0; u < PASSES; ++u) raw[u] = *(const u32x4_any*)(p + Q::N * (u * kThreads + (int)threadIdx.x));
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u) add(x[u]);
+    for (int u = 0; u < PASSES; ++u) {
+      const auto x = Q::widen(raw[u]);
+#pragma unroll
+      for (int j = 0; j < Q::N; j += 2) {
+        q0 = fma((double)x[j], (double)x[j], q0);
+        q1 = fma((double)x[j + 1], (double)x[j + 1], q1);
+      }
+    }
   } else {
     const int whole = n / 8;
     for (int i = threadIdx.x; i < whole; i += kThreads) add(R::load_raw(p + 8 * i));
@@ -118,13 +141,21 @@ __device__ __forceinline__ void chunk_clip(const void* in, void* out, int64_t fi
   typedef RowType<TYPE> R;
   const auto* p = (const typename R::T*)in + first;
   auto* o = (typename R::T*)out + first;
-  constexpr int PASSES = CHUNK / (kThreads * 8);
+  typedef Quad<TYPE> Q;
+  constexpr int PASSES = CHUNK / (kThreads * Q::N);
   if (n == CHUNK) {
-    typename R::Raw x[PASSES];
+    u32x4_any raw[PASSES];
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u) x[u] = R::load_raw(p + 8 * (u * kThreads + (int)threadIdx.x));
+    for (int u = 0; u < PASSES; ++u) raw[u] = *(const u32x4_any*)(p + Q::N * (u * kThreads + (int)threadIdx.x));
+    // Long lists go past the caches: 1.4 billion bf16 elements 1577 -> 1538 us, 150 million fp32 365 -> 341 (383 with the 32 bytes of
+    // eight elements a thread in two stores).  Short ones are left in them for what reads them next.
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u) R::store(o + 8 * (u * kThreads + (int)threadIdx.x), R::widen(x[u]) * factor);
+    for (int u = 0; u < PASSES; ++u) {
+      const u32x4_any y = Q::narrow(Q::widen(raw[u]) * factor);
+      auto* const to = (u32x4_any*)(o + Q::N * (u * kThreads + (int)threadIdx.x));
+      if constexpr (CHUNK == 1 << kGradChunkLog2) __builtin_nontemporal_store(y, to);
+      else *to = y;
+    }
   } else {
     const int whole = n / 8;
     for (int i = threadIdx.x; i < whole; i += kThreads) R::store(o + 8 * i, R::widen(R::load_raw(p + 8 * i)) * factor);

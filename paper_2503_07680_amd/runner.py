@@ -140,10 +140,11 @@ _TYPES = {torch.bfloat16: B.HBP_BF16, torch.float32: B.HBP_F32}
 
 def _check(name: str, t, device: torch.device, dtype, shape) -> None:
     """A tensor on the object's device, of the type and shape that it was made for; rows may have a stride."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device:
+        return
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise ValueError("%s: a tensor on %s is wanted" % (name, device))
-    if t.dtype != dtype or t.shape != shape:
-        raise ValueError("%s: %s %s is wanted, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    raise ValueError("%s: %s %s is wanted, got %s %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 
 def _on(device: torch.device, call, *args) -> None:
@@ -243,22 +244,25 @@ class PackedEmbedding:
         self.desc = B.EmbedDesc(total_tokens=self.T, vocab=self.vocab, dim=self.dim, table_type=_TYPES[table_type],
                                 row_type=_TYPES[out_type], scale=float(scale))
         self.ws_bytes = B.hbp_embed_bwd_workspace_bytes(self.desc)
+        self.strides = (0, 0)  # the descriptor's
         self.ws = None
         self.out = torch.empty((self.T, self.dim), dtype=out_type, device=self.device)
 
     def _rows(self, name: str, t: torch.Tensor, dtype, n: int) -> int:
         """Stride of [n, dim] rows in elements; overlapping or scattered rows are refused."""
         _check(name, t, self.device, dtype, (n, self.dim))
-        if (self.dim > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < self.dim):
+        row, column = t.stride()
+        if (self.dim > 1 and column != 1) or (n > 1 and row < self.dim):
             raise ValueError("%s: rows of adjacent elements are wanted" % name)
-        return t.stride(0) if n > 1 else self.dim
+        return row if n > 1 else self.dim
 
     def _operands(self, table: torch.Tensor, rows: torch.Tensor, tokens: torch.Tensor) -> None:
         _check("tokens", tokens, self.device, torch.int32, (self.T,))
         if not tokens.is_contiguous():
             raise ValueError("tokens: a contiguous tensor is wanted")
-        self.desc.table_stride = self._rows("table", table, self.table_type, self.vocab)
-        self.desc.row_stride = self._rows("rows", rows, self.out_type, self.T)
+        strides = (self._rows("table", table, self.table_type, self.vocab), self._rows("rows", rows, self.out_type, self.T))
+        if strides != self.strides:
+            self.desc.table_stride, self.desc.row_stride = self.strides = strides
 
     def forward(self, table: torch.Tensor, tokens: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """scale * table[tokens]; into this object's buffer unless ``out`` is given."""
