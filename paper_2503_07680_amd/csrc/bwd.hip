@@ -110,8 +110,8 @@ struct DqLds {
 };
 
 //
-// CROSS: cross attention.  An item is 128 folded rows (see Fold) of a query tile for one folded group of heads, which the place
-// in the grid names; HALVES = 2: the tile's 256, on shared tiles, item `block` of the launch.  Every row sees all keys of its
+// CROSS: cross attention.  An item is 128 folded rows (see Fold) of a query tile for one folded group of heads, HALVES = 2: the
+// tile's 256, on shared tiles; item `block` of the launch, or (block < 0) by the place in the grid.  Every row sees all keys of its
 // sample; with p.dq_parts > 1 these are dealt out in so many parts of whole key tiles, and the parts' sums of dQ are added up by
 // cross_reduce_dq_kernel.
 template <int DQK, int DV, int HALVES = 1, bool SHARED = false, bool DIRECT = HALVES == 2, bool CROSS = false>
@@ -177,18 +177,24 @@ __device__ __forceinline__ void dq_items(int block) {
   for (;;) {
     const BwdArgs& p = *bwd_args<!DIRECT>();
     const WorkQueues wq{p.counter_dq, p.n_q_tiles, p.Hkv * p.n_split_dq, quotient(p.g / (SHARED ? 2 : 1), p.n_split_dq)};
-    int tile_idx, h, key_part = 0;
+    int tile_idx, h, key_part = 0, row_half = 0;
     if constexpr (CROSS) {
       const int groups = p.Hkv * p.g;
-      if constexpr (HALVES == 1) {
+      if (block < 0) {  // by the place in the grid
         tile_idx = blockIdx.z;
         h = blockIdx.x;
         key_part = blockIdx.y >> 1;
+        row_half = blockIdx.y & 1;
       } else {
-        const int of_part = p.n_q_tiles * groups;
+        const int of_tile = groups * (2 / HALVES), of_part = p.n_q_tiles * of_tile;
         key_part = quotient(block, of_part);
-        tile_idx = quotient(block - key_part * of_part, groups);
-        h = block - key_part * of_part - tile_idx * groups;
+        const int rest = block - key_part * of_part;
+        tile_idx = quotient(rest, of_tile);
+        h = rest - tile_idx * of_tile;
+        if (HALVES == 1) {
+          row_half = h >= groups;
+          h -= row_half * groups;
+        }
       }
     } else if constexpr (!DIRECT) {
       if (!next_item(wq, (int*)smem, tid, q_cur, q_tried, tile_idx, h)) break;
@@ -210,7 +216,7 @@ __device__ __forceinline__ void dq_items(int block) {
       if (ok) {
         ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= 2 * BM >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
-             (HALVES == 2 || BM * (int)(blockIdx.y & 1) < (tl.row_end - tl.row_begin) << p.fold_log2);
+             (HALVES == 2 || BM * row_half < (tl.row_end - tl.row_begin) << p.fold_log2);
         if (ok && p.dq_parts > 1) {
           const int n = ks1 - ks0, per = ((n + p.dq_parts - 1) / p.dq_parts + BN - 1) / BN * BN, from = min((int64_t)per * key_part, (int64_t)n);
           ks1 = ks0 + from + min(n - from, per);
@@ -223,7 +229,7 @@ __device__ __forceinline__ void dq_items(int block) {
     }
     if (ok) {
       // CROSS: rows of the tile, folded, from 0 on
-      const int r0 = CROSS ? BM * (HALVES == 2 ? half : (int)(blockIdx.y & 1)) : tl.row_begin;
+      const int r0 = CROSS ? BM * (HALVES == 2 ? half : row_half) : tl.row_begin;
       const int r1 = CROSS ? min(r0 + BM, (tl.row_end - tl.row_begin) << p.fold_log2) : tl.row_end;
       const bool has_head = HALVES == 1 || SHARED || h < p.Hq;  // an odd number of heads: the last pair has one
       if (!has_head) h = p.Hq - 1;
@@ -1749,7 +1755,7 @@ int launch_bwd(int d_qk, int d_v, const BwdParams& p, int grid_dq, int grid_dkdv
 // Grids: folded groups of heads (kv heads times parts), halves of a query tile, tiles.
 template <int DQK, int DV>
 __global__ __launch_bounds__(kThreads, DQK <= 128 ? 2 : 1) void cross_dq_kernel(const BwdParams) {
-  dq_items<DQK, DV, 1, false, true, true>(0);
+  dq_items<DQK, DV, 1, false, true, true>(-1);
 }
 template <int DQK, int DV>
 __global__ __launch_bounds__(2 * kThreads, 2) void cross_dkdv_eight_kernel(const BwdParams) {
@@ -1765,6 +1771,13 @@ __global__ __launch_bounds__(2 * kThreads, 2) void cross_both_eight_kernel(const
   const int block = blockIdx.x;
   if (dq_first ? block >= n_dq : block < n_dkdv) dkdv8_items<DQK, DV, true, true>(dq_first ? block - n_dq : block, 1);
   else dq_items<DQK, DV, 2, true, true, true>(dq_first ? block : block - n_dkdv);
+}
+// The same at head size 192, workgroups of four wavefronts: dQ's items are halves of a tile.
+template <int DQK, int DV>
+__global__ __launch_bounds__(kThreads, 1) void cross_both_four_kernel(const BwdParams, int n_dkdv, int n_dq, int dq_first) {
+  const int block = blockIdx.x;
+  if (dq_first ? block >= n_dq : block < n_dkdv) dkdv_items<DQK, DV, true, true>(dq_first ? block - n_dq : block, 1);
+  else dq_items<DQK, DV, 1, false, true, true>(dq_first ? block : block - n_dkdv);
 }
 
 // dQ of a tile's rows from the parts' sums, in the parts' order.  DQK / 4 lanes a row; bound by reading the parts once.  Grid:
@@ -1824,23 +1837,23 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
-  bool one = false;
-  if constexpr (kEight) {
-    const int64_t n_dkdv = (int64_t)p.n_tiles * p.Hkv * p.n_split, n_dq = (int64_t)p.n_q_tiles * p.Hkv * p.g * p.dq_parts;
-    one = cross_one_launch(n_dkdv, n_dq);
-    if (one) {
-      constexpr int lds_both_dq = DqLds<DQK, DV, 2, true>::BYTES, lds = lds_both_dq > lds_dkdv ? lds_both_dq : lds_dkdv;
-      static bool both_set = false;
-      if (!both_set) {
-        e = hipFuncSetAttribute((const void*)cross_both_eight_kernel<DQK, DV>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return (int)e;
-        both_set = true;
-      }
-      hipLaunchKernelGGL((cross_both_eight_kernel<DQK, DV>), dim3((unsigned)(n_dkdv + n_dq)), dim3(2 * kThreads), lds, s, p, (int)n_dkdv, (int)n_dq,
-                         (int)cross_dq_first(p.T, p.Tk, (p.Hq / p.Hkv), p.n_split, p.dq_parts));
-      e = hipGetLastError();
+  const int64_t n_dkdv = (int64_t)p.n_tiles * p.Hkv * p.n_split, n_dq = (int64_t)p.n_q_tiles * p.Hkv * p.g * p.dq_parts * (kEight ? 1 : 2);
+  const bool one = cross_one_launch(n_dkdv, n_dq);
+  if (one) {
+    constexpr int lds_both_dq = DqLds<DQK, DV, kEight ? 2 : 1, kEight>::BYTES, lds = lds_both_dq > lds_dkdv ? lds_both_dq : lds_dkdv;
+    void (*both)(const BwdParams, int, int, int);
+    if constexpr (kEight) both = cross_both_eight_kernel<DQK, DV>;
+    else both = cross_both_four_kernel<DQK, DV>;
+    static bool both_set = false;
+    if (!both_set) {
+      e = hipFuncSetAttribute((const void*)both, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return (int)e;
+      both_set = true;
     }
+    hipLaunchKernelGGL(both, dim3((unsigned)(n_dkdv + n_dq)), dim3(kEight ? 2 * kThreads : kThreads), lds, s, p, (int)n_dkdv, (int)n_dq,
+                       (int)cross_dq_first(p.T, p.Tk, (p.Hq / p.Hkv), p.n_split, p.dq_parts));
+    e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
   }
   for (int at = 0; at < p.n_tiles && !one; at += kCrossMostTiles) {
     BwdParams part = p;

@@ -120,9 +120,9 @@ inline bool cross_dq_first(int64_t queries, int64_t keys, int group, int parts, 
   return keys * 3 * 256 / dq_parts > queries * group * 4 * 128 / parts;
 }
 
-// dK/dV and dQ in one launch, a workgroup of eight wavefronts an item, as long as the items' numbers stay exact in the kernel's
-// quotients (head sizes 64 and 128; at 192 the two have a launch each).  Against two launches, 56 packs of 550 to 19600 tokens a
-// side, 1/1 to 64/8 heads: 1.3 to 1.6 where the launches have few rounds, 1.0 to 1.1 in large packs, .99 at worst.
+// dK/dV and dQ in one launch, a workgroup an item, as long as the items' numbers stay exact in the kernel's quotients.  Against two
+// launches, 77 packs of 40 to 19600 tokens a side, 4/4 to 128/128 heads: 1.1 to 1.6 where the launches have few rounds, 1.0 to 1.1 in
+// large packs, .99 at worst.
 inline bool cross_one_launch(int64_t n_dkdv, int64_t n_dq) { return n_dkdv > 0 && n_dq > 0 && n_dkdv + n_dq < (1 << 22); }
 
 struct CrossBwdLayout {
