@@ -19,6 +19,7 @@
 
 #include "common.hpp"
 #include "cross_rules.hpp"
+#include "lds_limit.hpp"
 
 namespace hbp {
 
@@ -1819,14 +1820,9 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
   void (*dkdv)(const BwdParams);
   if constexpr (kEight) dkdv = cross_dkdv_eight_kernel<DQK, DV>;
   else dkdv = cross_dkdv_four_kernel<DQK, DV>;
-  static bool attr_set = false;
-  if (!attr_set) {
-    hipError_t e = hipFuncSetAttribute((const void*)cross_dq_kernel<DQK, DV>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_dq);
-    if (e != hipSuccess) return (int)e;
-    e = hipFuncSetAttribute((const void*)dkdv, hipFuncAttributeMaxDynamicSharedMemorySize, lds_dkdv);
-    if (e != hipSuccess) return (int)e;
-    attr_set = true;
-  }
+  static LdsLimitDone dq_done, dkdv_done, both_done;
+  if (const int e = raise_lds_limit((const void*)cross_dq_kernel<DQK, DV>, lds_dq, dq_done)) return e;
+  if (const int e = raise_lds_limit((const void*)dkdv, lds_dkdv, dkdv_done)) return e;
   hipError_t e = hipSuccess;
   if (p.T > 0) {
     const bool small = (int64_t)p.T * p.Hq <= kPreSmall;
@@ -1844,12 +1840,7 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     void (*both)(const BwdParams, int, int, int);
     if constexpr (kEight) both = cross_both_eight_kernel<DQK, DV>;
     else both = cross_both_four_kernel<DQK, DV>;
-    static bool both_set = false;
-    if (!both_set) {
-      e = hipFuncSetAttribute((const void*)both, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (e != hipSuccess) return (int)e;
-      both_set = true;
-    }
+    if (const int err = raise_lds_limit((const void*)both, lds, both_done)) return err;
     hipLaunchKernelGGL(both, dim3((unsigned)(n_dkdv + n_dq)), dim3(kEight ? 2 * kThreads : kThreads), lds, s, p, (int)n_dkdv, (int)n_dq,
                        (int)cross_dq_first(p.T, p.Tk, (p.Hq / p.Hkv), p.n_split, p.dq_parts));
     e = hipGetLastError();

@@ -12,6 +12,7 @@
 // The sort is one launch (embed_group_kernel): a workgroup owns a range of up to 1024 ids, reads all tokens twice (32 KB to 1 MB,
 // from its die's L2), counts those below its range, which is where its part of the order begins, and places its own.  It
 // also zeroes those rows of a fresh dW that have no token.  Very many tokens or ids take a radix sort of nine bits a pass instead.
+#include "lds_limit.hpp"
 #include "rows.hpp"
 
 namespace hbp {
@@ -582,12 +583,8 @@ int sums(const EmbedParams& p, const Sorted& srt, const void* d_out, void* d_tab
 }
 
 int group(const EmbedParams& p, int bins, uint32_t* keys, uint32_t* order, const Fill& fill, hipStream_t s) {
-  static bool attr_set = false;
-  if (!attr_set) {
-    const hipError_t e = hipFuncSetAttribute((const void*)embed_group_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GroupLds));
-    if (e != hipSuccess) return (int)e;
-    attr_set = true;
-  }
+  static LdsLimitDone done;
+  if (const int e = raise_lds_limit((const void*)embed_group_kernel, (int)sizeof(GroupLds), done)) return e;
   hipLaunchKernelGGL(embed_group_kernel, dim3((unsigned)((p.V + (int64_t)bins - 1) / bins)), dim3(kSortThreads), sizeof(GroupLds), s, p.tokens, p.T, p.V, bins,
                      keys, order, fill);
   return (int)hipGetLastError();

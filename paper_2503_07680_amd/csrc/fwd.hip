@@ -29,6 +29,7 @@
 
 #include "common.hpp"
 #include "cross_rules.hpp"
+#include "lds_limit.hpp"
 
 namespace hbp {
 
@@ -798,12 +799,8 @@ int launch_fwd(int d_qk, int d_v, const FwdParams& p, int tile_rows, hipStream_t
 template <int DQK, int DV, int TP>
 static int launch_cross_fwd_t(FwdParams p, hipStream_t s) {
   constexpr int lds_bytes = FwdLds<DQK, DV, 4 * TP>::bytes();
-  static bool attr_set = false;
-  if (!attr_set) {
-    const hipError_t e = hipFuncSetAttribute((const void*)cross_forward_kernel<DQK, DV, TP>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-    if (e != hipSuccess) return (int)e;
-    attr_set = true;
-  }
+  static LdsLimitDone done;
+  if (const int e = raise_lds_limit((const void*)cross_forward_kernel<DQK, DV, TP>, lds_bytes, done)) return e;
   p.halves = TP == 1;
   p.n_split = 1;
   constexpr int kMost = 32767;  // the tiles, or halves of them, are the grid's third dimension

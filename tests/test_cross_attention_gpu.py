@@ -163,6 +163,56 @@ def test_tiles_that_do_not_fit_are_skipped(kl):
     assert all(torch.equal(getattr(a, n), t) for n, t in good.items())
 
 
+def test_nothing_to_do():
+    from paper_2503_07680_amd.runner import PackedCrossAttention
+    for ql, kl in (([], []), ([0, 0], [0, 0]), ([0], [5]), ([5], [0])):
+        a = PackedCrossAttention(ql, kl, 4, 2, 64, 64)
+        x = inputs(ql, kl, 4, 2, 64, 64, 1)
+        o, lse = a.forward(*x[:3])
+        a.alloc_backward()
+        for t in (a.dq, a.dk, a.dv):
+            t.fill_(5.0)
+        a.backward(*x)
+        assert bool((o == 0).all()) and bool(torch.isinf(lse).all())
+        assert all(bool((t == 0).all()) for t in (a.dq, a.dk, a.dv))
+
+
+def test_what_the_runner_refuses():
+    from paper_2503_07680_amd.runner import GradientClip, PackedCrossAttention, PackedEmbedding
+    ql, kl = [30, 5], [40, 9]
+    a = PackedCrossAttention(ql, kl, 4, 2, 64, 64)
+    q, k, v, d_o = inputs(ql, kl, 4, 2, 64, 64, 2)
+    wrong = [(q.float(), k, v), (q[:-1], k, v), (q, k.cpu(), v), (q, k, v[:, :1]), (q.transpose(0, 1).contiguous().transpose(0, 1), k, v), (q, None, v)]
+    for x in wrong:
+        with pytest.raises(ValueError):
+            a.forward(*x)
+        with pytest.raises(ValueError):
+            a.backward(*x, d_o)
+    with pytest.raises(ValueError):
+        a.backward(q, k, v, d_o[1:])
+    e = PackedEmbedding(10, 50, 16)
+    w, t = torch.zeros(50, 16, dtype=torch.bfloat16, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda")
+    rows = torch.zeros(10, 16, dtype=torch.bfloat16, device="cuda")
+    for x in ((w.float(), t), (w[:49], t), (w, t.long()), (w, t[:9]), (w, t.repeat(2)[::2]), (w.t().contiguous().t(), t), (w[:1].expand(50, 16), t)):
+        with pytest.raises(ValueError):
+            e.forward(*x)
+        with pytest.raises(ValueError):
+            e.backward(rows, x[1], x[0])
+    with pytest.raises(ValueError):
+        e.backward(rows[:9], t, w)
+    for bad in ([w.half()], [w.cpu()], [w.t()]):
+        with pytest.raises(ValueError):
+            GradientClip(bad)
+    with pytest.raises(ValueError):
+        GradientClip([w], [w.float()])
+    with pytest.raises(ValueError):
+        GradientClip([w], [])
+    for bad in ([w, w], [w, w[3:4]]):
+        with pytest.raises(Exception) as err:
+            GradientClip(bad).clip(1.0)
+        assert err.value.status == 1
+
+
 def test_captured_and_on_another_stream():
     from paper_2503_07680_amd.runner import PackedCrossAttention
     ql, kl = [300, 0, 64, 1200], [90, 20, 0, 70]
