@@ -10,6 +10,8 @@
  *  - Plain C.  Every function returns an hbp_status (0 = HBP_OK) and never throws or aborts.
  *  - The caller owns every buffer.  The library allocates no device memory, never
  *    synchronises the device and uses only the caller's workspace for scratch.
+ *    A workspace serves one call at a time: calls that may overlap (other streams, graphs that replay beside each other)
+ *    need one each.
  *  - "host" / "device" on a pointer says where the memory must live.
  *  - Device entry points enqueue work on the caller's HIP stream (a hipStream_t passed as
  *    void*; NULL = the default stream) and return without waiting.
@@ -411,7 +413,7 @@ hbp_status hbp_packed_ce(const void* logits, int64_t logit_stride_t, int32_t tot
  * Layouts, head dims and strides as in hbp_attn_desc: Q [Tq,Hq,d_qk], K [Tk,Hkv,d_qk], V [Tk,Hkv,d_v], O/dO [Tq,Hq,d_v],
  * LSE [Hq,Tq] fp32 dense. */
 typedef struct {
-  int32_t total_queries, total_keys, n_samples;
+  int32_t total_queries, total_keys, n_samples; /* up to 2^31 - 4097 keys, and query rows times the heads that share a stream */
   int32_t n_q_heads, n_kv_heads;
   int32_t d_qk, d_v;
   float softmax_scale; /* <= 0: 1/sqrt(d_qk) */
@@ -449,6 +451,7 @@ hbp_status hbp_cross_workspace_bytes(const hbp_cross_desc* desc, int32_t which, 
  * Precision as hbp_varlen_attn_fwd (bf16 MFMA, fp32 accumulation and statistics, probabilities rounded to bf16 in front of
  * the product with V).  q_tiles: the HBP_TILES_QUERY list of hbp_cross_plan made with hbp_cross_tile_rows(..., HBP_FWD).
  * Malformed tiles are skipped, rows in no tile left untouched.  No tiles: no-op.  All pointers but desc: DEVICE.
+ * What is not finite in a sample spoils rows of that sample alone, in the backward too.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, DEVICE, by the rules of hbp_varlen_attn_fwd (k and v may be null where
  * there are no keys); nothing is launched then.
  */

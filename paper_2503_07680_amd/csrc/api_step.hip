@@ -92,6 +92,7 @@ bool overlaps(const void* const* in, void* const* out, const int64_t* sizes, con
   return false;
 }
 
+constexpr int64_t kMaxRows = INT32_MAX - 4096;  // rounding up to whole tiles and parts stays in 32 bits
 constexpr int64_t kMaxTokenStride = int64_t{1} << 22;  // elements: rows of a tile are addressed in 32 bits, as in hbp_varlen_attn_*
 
 hbp_status check_cross(const hbp_cross_desc* d) {
@@ -106,7 +107,8 @@ hbp_status check_cross(const hbp_cross_desc* d) {
   for (int i = 0; i < 4; ++i)
     if (t[i] % 8 || h[i] % 8 || t[i] < dim[i] || h[i] < dim[i] || t[i] > kMaxTokenStride) return HBP_ERR_SHAPE;
   // the kernels count folded rows, and steps over them, in 32 bits
-  if (((int64_t)d->total_queries << hbp::cross_fold_log2(*d)) > INT32_MAX || (int64_t)d->total_queries * d->n_q_heads > ((int64_t)1 << 36))
+  if (((int64_t)d->total_queries << hbp::cross_fold_log2(*d)) > kMaxRows || d->total_keys > kMaxRows ||
+      (int64_t)d->total_queries * d->n_q_heads > ((int64_t)1 << 36))
     return HBP_ERR_UNSUPPORTED;
   return HBP_OK;
 }

@@ -220,13 +220,17 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
   l.place[tid] = 0;
   __syncthreads();
   uint32_t below = 0;  // of this wavefront
-  for (int i0 = wave * 256; i0 < T; i0 += kSortWaves * 256) {
-    const i32x4_any t = load_tokens(tokens, T, i0 + lane * 4);
+  for (int i0 = wave * 256; i0 < T; i0 += 4 * kSortWaves * 256) {
+    i32x4_any t[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      below += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)t[j] < (uint32_t)lo));
-      if (of_mine(t[j])) atomicAdd(&l.place[t[j] - lo], 1u);  // whole numbers: the order does not matter
-    }
+    for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, T, i0 + k * kSortWaves * 256 + lane * 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        below += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)t[k][j] < (uint32_t)lo));
+        if (of_mine(t[k][j])) atomicAdd(&l.place[t[k][j] - lo], 1u);  // whole numbers: the order does not matter
+      }
   }
   if (lane == 0) l.below[wave] = below;
   __syncthreads();
@@ -540,7 +544,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, 
   if (ADD) had = RawSpan<TABLE, VEC>(row + at.col);
   const float* part = s.part + (int64_t)c * 2 * p.dim + at.col;
   f32x8_row acc = load_span<HBP_F32, VEC>(part + p.dim);
-  constexpr int U = 8;
+  constexpr int U = 16;
   for (int i = 1; i <= n; i += U) {
     f32x8_row x[U];
 #pragma unroll

@@ -162,10 +162,10 @@ static hbp_status hbp_cross_plan_impl(const int32_t* q_lengths, const int32_t* k
     if (q_lengths[i] < 0 || kv_lengths[i] < 0) return HBP_ERR_INVALID_ARG;
     at_q += q_lengths[i];
     at_kv += kv_lengths[i];
+    if (at_q > INT32_MAX || at_kv > INT32_MAX) return HBP_ERR_INVALID_ARG;
     pairs += (int64_t)q_lengths[i] * kv_lengths[i];
     n_tiles += ((int64_t)(queries ? q_lengths[i] : kv_lengths[i]) + tile_rows - 1) / tile_rows;
   }
-  if (at_q > INT32_MAX || at_kv > INT32_MAX) return HBP_ERR_INVALID_ARG;
   std::vector<Item> items;
   items.reserve((size_t)n_tiles);
   int64_t at = 0;

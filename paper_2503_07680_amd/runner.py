@@ -245,8 +245,7 @@ class PackedEmbedding:
                                 row_type=_TYPES[out_type], scale=float(scale))
         self.ws_bytes = B.hbp_embed_bwd_workspace_bytes(self.desc)
         self.strides = (0, 0)  # the descriptor's
-        self.ws = None
-        self.out = torch.empty((self.T, self.dim), dtype=out_type, device=self.device)
+        self.ws = self.out = None
 
     def _rows(self, name: str, t: torch.Tensor, dtype, n: int) -> int:
         """Stride of [n, dim] rows in elements; overlapping or scattered rows are refused."""
@@ -266,7 +265,10 @@ class PackedEmbedding:
 
     def forward(self, table: torch.Tensor, tokens: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """scale * table[tokens]; into this object's buffer unless ``out`` is given."""
-        out = self.out if out is None else out
+        if out is None:
+            if self.out is None:
+                self.out = torch.empty((self.T, self.dim), dtype=self.out_type, device=self.device)
+            out = self.out
         self._operands(table, out, tokens)
         _on(self.device, B.hbp_embed_fwd, self.desc, table, tokens, out)
         return out

@@ -74,7 +74,7 @@ def test_rows_of_a_query_tile(hq, hkv, fold):
     (dict(n_q_heads=7), 2), (dict(d_qk=96), 3), (dict(d_v=64), 3), (dict(total_queries=-1), 1), (dict(total_keys=-1), 1),
     (dict(n_samples=-1), 1), (dict(n_kv_heads=0), 1), (dict(softmax_scale=float("nan")), 1), (dict(q_stride_h=64), 2),
     (dict(k_stride_t=100), 2), (dict(v_stride_t=-256), 2), (dict(o_stride_t=(1 << 22) + 8), 2),
-    (dict(total_queries=1 << 30, n_q_heads=64), 3),
+    (dict(total_queries=1 << 30, n_q_heads=64), 3), (dict(total_keys=2 ** 31 - 1), 3),
 ])
 def test_descriptors(kw, status):
     lib, d = H.load_library(), desc(**kw)
