@@ -22,7 +22,8 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kGroupTile = 16384, kGroupBins = 1024;  // tokens that are placed at a time, ids of a workgroup (embed_group_kernel)
+constexpr int kGroupList = 12288, kGroupBins = 1024;  // tokens that are placed at a time, ids of a workgroup (embed_group_kernel)
+constexpr int kWaveList = kGroupList / 16;           // of each of its wavefronts
 constexpr int kTileRounds = 4, kTile = kTileRounds * kSortThreads;  // of each workgroup where there are more
 constexpr int kSmallChunks = 16384;          // up to so many tokens: chunks of 16, else of 32
 constexpr uint32_t kNoKey = 0xffffffffu;
@@ -189,24 +190,27 @@ __device__ __forceinline__ void fill_rows(const Fill& f, int block) {
   for (int64_t r = from + wave; r < to; r += waves) zero_row(f, r, lane);
 }
 
-// The one-launch sort: workgroup w owns the ids [w bins, (w + 1) bins).  First all tokens are read for the numbers of each of its
-// ids and of all smaller ones; then again, kGroupTile at a time, for their places: the tile's tokens of its ids are listed in
-// LDS in order, a wavefront ranks 64 listed ones among those of the same id by ballots over the bits, and the counts of the
-// wavefronts in front, of the tiles in front and of the smaller ids make up the rest of a place.
-// 8192 tokens, 128256 ids: 26.8 us with one workgroup sorting 9 bits at a time in LDS.
+// The one-launch sort: workgroup w owns the ids [w bins, (w + 1) bins), and each of its wavefronts reads a stretch of the tokens,
+// counts those of each of its ids and of all smaller ones and lists the former in LDS, in order.  A wavefront then ranks 64 listed
+// ones at a time among those of the same id by ballots over the bits; the counts of the wavefronts in front and of the smaller ids
+// make up the rest of a place.  Bound by the instructions of the scan, some 13 a token of a lane.  Where a few ids have so many of
+// the tokens that a wavefront's part of the list is too short, all are read again, for kGroupList places of the whole list at a time.
+// 65536 tokens, 32000 ids, us: tiles of 16384 tokens listed one after the other in a second reading 28, the whole stretch in a second
+// reading 24, in the first 21; 8192 tokens, 128256 ids: 26.8 with one workgroup that sorts nine bits at a time in LDS, 7.5.
 struct GroupLds {
-  uint16_t counts[kGroupBins * kSortWaves];  // of the tile, [id][wavefront]
-  uint16_t id[kGroupTile], pos[kGroupTile], rank[kGroupTile];
+  uint16_t counts[kGroupBins * kSortWaves];  // of the listed tokens, [id][wavefront]
+  uint16_t id[kGroupList], rank[kGroupList];
+  uint32_t pos[kGroupList];
   uint32_t place[kGroupBins];                // counts, then the next place, of each id
-  uint32_t sums[kSortWaves], below[kSortWaves];
+  uint32_t sums[kSortWaves], below[kSortWaves], mine[kSortWaves];
   uint64_t has[kSortWaves];                  // ids with a token, a bit each
 };
 typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ i32x4_any load_tokens(const int32_t* tokens, int T, int i) {  // -1 behind the last
-  if (i + 4 <= T) return *(const i32x4_any*)(tokens + i);
+__device__ __forceinline__ i32x4_any load_tokens(const int32_t* tokens, int end, int i) {  // -1 from end on
+  if (i + 4 <= end) return *(const i32x4_any*)(tokens + i);
   i32x4_any t;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) t[j] = i + j < T ? tokens[i + j] : -1;
+  for (int j = 0; j < 4; ++j) t[j] = i + j < end ? tokens[i + j] : -1;
   return t;
 }
 __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t* tokens, int T, int V, int bins, uint32_t* keys,
@@ -214,82 +218,97 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
   extern __shared__ __attribute__((aligned(16))) char group_lds[];
   GroupLds& l = *(GroupLds*)group_lds;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int lo = (int)((int64_t)blockIdx.x * bins), mine = min(bins, V - lo);
+  const int lo = (int)((int64_t)blockIdx.x * bins), own_ids = min(bins, V - lo);
   const uint64_t in_front = ((uint64_t)1 << lane) - 1;
-  auto of_mine = [&](int t) { return (uint32_t)(t - lo) < (uint32_t)mine; };  // tokens that are none are below 0 or from V on
+  auto of_mine = [&](int t) { return (uint32_t)(t - lo) < (uint32_t)own_ids; };  // tokens that are none are below 0 or from V on
+  // A lane's four tokens from position pos on into the list: the wavefront's first one goes to place at; nothing to place `limit` or
+  // behind it, nor to one below 0.  Returns how many of the wavefront's tokens there are.
+  auto list = [&](const i32x4_any& t, int pos, uint32_t at, uint32_t limit, auto each) {
+    uint64_t b[4];
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      b[j] = __builtin_amdgcn_ballot_w64(of_mine(t[j]));
+      n += (uint32_t)__popcll(b[j]);
+    }
+    if (n == 0) return 0u;
+    uint32_t to = at;  // of this lane's first: the lanes in front, four tokens each
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to += (uint32_t)__popcll(b[j] & in_front);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (of_mine(t[j])) {
+        each((uint32_t)(t[j] - lo));
+        if (to < limit) {
+          l.id[to] = (uint16_t)(t[j] - lo);
+          l.pos[to] = (uint32_t)(pos + j);
+        }
+        ++to;
+      }
+    return n;
+  };
+  const int stretch = (T + kSortWaves * 256 - 1) / (kSortWaves * 256) * 256, begin = wave * stretch, end = min(begin + stretch, T);
   l.place[tid] = 0;
   __syncthreads();
-  uint32_t below = 0;  // of this wavefront
-  for (int i0 = wave * 256; i0 < T; i0 += 4 * kSortWaves * 256) {
+  uint32_t below = 0, mine = 0;  // of this wavefront
+  for (int i0 = begin; i0 < end; i0 += 1024) {
     i32x4_any t[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, T, i0 + k * kSortWaves * 256 + lane * 4);
+    for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, end, i0 + k * 256 + lane * 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         below += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)t[k][j] < (uint32_t)lo));
-        if (of_mine(t[k][j])) atomicAdd(&l.place[t[k][j] - lo], 1u);  // whole numbers: the order does not matter
       }
-  }
-  if (lane == 0) l.below[wave] = below;
-  __syncthreads();
-  const uint32_t own = l.place[tid];
-  const uint64_t has = __builtin_amdgcn_ballot_w64(own != 0);
-  if (lane == 0) l.has[wave] = has;
-  uint32_t base = 0;
-  for (int w = 0; w < kSortWaves; ++w) base += l.below[w];
-  const uint32_t place = base + before_me(own, l.sums);
-  __syncthreads();
-  l.place[tid] = place;
-  const uint32_t end = __builtin_amdgcn_readfirstlane(base + l.sums[0] + l.sums[1] + l.sums[2] + l.sums[3] + l.sums[4] + l.sums[5] + l.sums[6] + l.sums[7] +
-                                                      l.sums[8] + l.sums[9] + l.sums[10] + l.sums[11] + l.sums[12] + l.sums[13] + l.sums[14] + l.sums[15]);
-  i32x4_any next[4];  // the wavefront's 1024 tokens of the next tile
-#pragma unroll
-  for (int k = 0; k < 4; ++k) next[k] = load_tokens(tokens, T, wave * 1024 + k * 256 + lane * 4);
-  for (int t0 = 0; t0 < T; t0 += kGroupTile) {
-    i32x4_any t[4];
-    uint32_t listed = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      t[k] = next[k];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) listed += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(of_mine(t[k][j])));
-      next[k] = load_tokens(tokens, T, t0 + kGroupTile + wave * 1024 + k * 256 + lane * 4);
+      mine += list(t[k], i0 + k * 256 + lane * 4, wave * kWaveList + mine, (wave + 1) * kWaveList, [&](uint32_t id) {
+        atomicAdd(&l.place[id], 1u);  // whole numbers: the order does not matter
+      });
     }
-    __syncthreads();  // the tile before is placed
+  }
+  if (lane == 0) {
+    l.below[wave] = below;
+    l.mine[wave] = mine;
+  }
+  __syncthreads();
+  const uint32_t of_id = l.place[tid];
+  const uint64_t has = __builtin_amdgcn_ballot_w64(of_id != 0);
+  if (lane == 0) l.has[wave] = has;
+  // places in front of this range; this wavefront's first place in the whole list; its length; the longest part
+  uint32_t base = 0, list_at = 0, all = 0, longest = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    base += l.below[w];
+    list_at += w < wave ? l.mine[w] : 0;
+    all += l.mine[w];
+    longest = max(longest, l.mine[w]);
+  }
+  const uint32_t place = base + before_me(of_id, l.sums);
+  __syncthreads();
+  l.place[tid] = place;
+  all = __builtin_amdgcn_readfirstlane(all);
+  list_at = __builtin_amdgcn_readfirstlane(list_at);
+  const bool again = __builtin_amdgcn_readfirstlane(longest) > kWaveList;  // the list is made in pieces of the whole
+  for (uint32_t from = 0; from < all; from += again ? kGroupList : all) {
+    if (from > 0) __syncthreads();  // what was listed before has its places
     for (int i = tid; i < kGroupBins * kSortWaves / 8; i += kSortThreads) ((u32x4_any*)l.counts)[i] = u32x4_any{0, 0, 0, 0};
-    if (lane == 0) l.sums[wave] = listed;
-    __syncthreads();
-    uint32_t at = 0, n = 0;
-    for (int w = 0; w < kSortWaves; ++w) {
-      if (w < wave) at += l.sums[w];
-      n += l.sums[w];
-    }
-    n = __builtin_amdgcn_readfirstlane(n);
-    if (n == 0) continue;
-    if (listed) {
+    if (again && mine > 0 && list_at < from + kGroupList && list_at + mine > from) {
+      uint32_t at = list_at - from;  // may be below 0: such places are compared as large ones
+      for (int i0 = begin; i0 < end; i0 += 1024) {
+        i32x4_any t[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint64_t b[4];
-        uint32_t to = at;  // of this lane's first: the lanes in front, four tokens each
+        for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, end, i0 + k * 256 + lane * 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          b[j] = __builtin_amdgcn_ballot_w64(of_mine(t[k][j]));
-          to += (uint32_t)__popcll(b[j] & in_front);
-          at += (uint32_t)__popcll(b[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (of_mine(t[k][j])) {
-            l.id[to] = (uint16_t)(t[k][j] - lo);
-            l.pos[to] = (uint16_t)(wave * 1024 + k * 256 + lane * 4 + j);
-            ++to;
-          }
+        for (int k = 0; k < 4; ++k) at += list(t[k], i0 + k * 256 + lane * 4, at, kGroupList, [](uint32_t) {});
       }
     }
     __syncthreads();
-    const int rounds = (int)((n + kSortThreads - 1) / kSortThreads), first = wave * rounds * 64 + lane;
+    // the listed ones that this wavefront places: entries first, first + 64, ... below n
+    const uint32_t n = again ? min(all - from, (uint32_t)kGroupList) : wave * kWaveList + mine;
+    const int rounds = again ? (int)((n + kSortThreads - 1) / kSortThreads) : (int)(mine + 63) / 64;
+    const int first = (again ? wave * rounds * 64 : wave * kWaveList) + lane;
     volatile uint16_t* const counts = l.counts;
     for (int e = 0; e < rounds; ++e) {
       const uint32_t i = first + e * 64;
@@ -319,9 +338,9 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) to += w < wave ? l.counts[d * kSortWaves + w] : 0;
       keys[to] = (uint32_t)lo + d;
-      order[to] = (uint32_t)t0 + l.pos[i];
+      order[to] = l.pos[i];
     }
-    if (t0 + kGroupTile < T) {
+    if (again && from + kGroupList < all) {
       __syncthreads();
       for (int e = 0; e < rounds; ++e) {
         const uint32_t i = first + e * 64;
@@ -330,9 +349,9 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
     }
   }
   if ((int)blockIdx.x == (int)gridDim.x - 1)  // behind the last token: none
-    for (int64_t i = (int64_t)end + tid; i < T; i += kSortThreads) keys[i] = (uint32_t)V;
+    for (int64_t i = (int64_t)base + all + tid; i < T; i += kSortThreads) keys[i] = (uint32_t)V;
   if (fill.blocks) {
-    for (int r = wave; r < mine; r += kSortWaves)
+    for (int r = wave; r < own_ids; r += kSortWaves)
       if (!(l.has[r >> 6] >> (r & 63) & 1)) zero_row(fill, lo + r, lane);
   }
 }
