@@ -15,6 +15,8 @@
 //                   dV^T += dO^T P,  dK^T += Q^T dS        (transposing LDS reads of dO and Q)
 // No atomics: dQ has its own pass (S and dP are recomputed there), so every output is written
 // once and the results are bit-stable from run to run.
+// Cross attention (hbp_cross_attn_bwd) runs the same items without the diagonal and with the query heads of a kv head folded
+// into rows (CROSS; cross_*_kernel at the end of the file).
 #include <type_traits>
 
 #include "common.hpp"
