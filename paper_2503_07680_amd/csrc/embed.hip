@@ -9,9 +9,13 @@
 // that a frequent id costs no workgroup more than the others: a run of equal ids inside a chunk is summed and written, of one
 // that goes beyond it the chunk's part is kept; (3) the parts of such runs are added up in the chunks' order.
 //
-// The sort is one launch (embed_group_kernel): a workgroup owns a range of up to 1024 ids, reads all tokens twice (32 KB to 1 MB,
-// from its die's L2), counts those below its range, which is where its part of the order begins, and places its own.  It
-// also zeroes those rows of a fresh dW that have no token.  Very many tokens or ids take a radix sort of nine bits a pass instead.
+// The sort is one launch (embed_group_kernel): a workgroup owns a range of up to 1024 ids, reads all tokens (4 KB to 1 MB, from
+// its die's L2; again where a few of its ids have very many), counts those below its range, which is where its part of the order
+// begins, and places its own.  It also zeroes those rows of a fresh dW that have no token.  Very many tokens or ids take a radix
+// sort of nine bits a pass instead.
+//
+// 8192 tokens, width 4096, added to a bf16 table of 128256 rows: 40 us (sort 7.4, sums 23 at 4.2 TB/s, joined runs 6);
+// 32767 tokens of width 2056, fresh fp32 table of 32000 rows: 121 (sort and zeros 54, sums 51, joined runs 11).
 #include "lds_limit.hpp"
 #include "rows.hpp"
 
@@ -485,6 +489,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, S
   const int c = (int)(w / wpr), lane = threadIdx.x & 63, n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
   const int v = (int)(w - (int64_t)c * wpr) * 64 + lane;
   if (c >= s.n_chunks) return;
+  const bool mine = v < n_vec;  // the other lanes stay: their registers hold ids and places too
   const int first = c * s.chunk, m = min(s.chunk, p.T - first);
   // lane l: entry l - 1 of the chunk
   const int i = first - 1 + lane;
@@ -499,12 +504,12 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, S
   const uint32_t before = __shfl_up(key, 1, 64);
   const uint64_t begins = __builtin_amdgcn_ballot_w64(lane >= 1 && lane <= n && key != before) >> 1;  // bit e: entry e begins a run
   const bool goes_on = n == m && __builtin_amdgcn_readlane(key, m + 1) == __builtin_amdgcn_readlane(key, m);
-  if (v >= n_vec) return;
-  const Span at = span_of<VEC>(v, p.dim);
+  const Span at = span_of<VEC>(min(v, n_vec - 1), p.dim);
   bool from_before = !(begins & 1);
   f32x8_row acc = {}, old = {};
   uint32_t cur = __builtin_amdgcn_readlane(key, 1);
   auto end_run = [&](bool goes_on) {
+    if (!mine) return;
     if (from_before || goes_on) put_part<VEC>(s.part + ((int64_t)c * 2 + (from_before ? 0 : 1)) * p.dim + at.col, acc);
     else store_span<TABLE, VEC>(d_table + (int64_t)cur * p.table_st, at, ADD ? old + acc * p.scale : acc * p.scale);
   };
