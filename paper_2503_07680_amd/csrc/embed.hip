@@ -10,12 +10,12 @@
 // that goes beyond it the chunk's part is kept; (3) the parts of such runs are added up in the chunks' order.
 //
 // The sort is one launch (embed_group_kernel): a workgroup owns a range of up to 1024 ids, reads all tokens (4 KB to 1 MB, from
-// its die's L2; again where a few of its ids have very many), counts those below its range, which is where its part of the order
+// its die's L2; twice again where a few of its ids have very many), counts those below its range, which is where its part of the order
 // begins, and places its own.  It also zeroes those rows of a fresh dW that have no token.  Very many tokens or ids take a radix
 // sort of nine bits a pass instead.
 //
 // 8192 tokens, width 4096, added to a bf16 table of 128256 rows: 40 us (sort 7.4, sums 23 at 4.2 TB/s, joined runs 6);
-// 32767 tokens of width 2056, fresh fp32 table of 32000 rows: 121 (sort and zeros 54, sums 51, joined runs 11).
+// 32767 tokens of width 2056, fresh fp32 table of 32000 rows: 106 (sort and zeros 44, sums 51, joined runs 8).
 #include "lds_limit.hpp"
 #include "rows.hpp"
 
@@ -26,7 +26,7 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kGroupList = 12288, kGroupBins = 1024;  // tokens that are placed at a time, ids of a workgroup (embed_group_kernel)
+constexpr int kGroupList = 12288, kGroupBins = 1024;  // tokens that a workgroup lists, ids of it (embed_group_kernel)
 constexpr int kWaveList = kGroupList / 16;           // of each of its wavefronts
 constexpr int kTileRounds = 4, kTile = kTileRounds * kSortThreads;  // of each workgroup where there are more
 constexpr int kSmallChunks = 16384;          // up to so many tokens: chunks of 16, else of 32
@@ -173,38 +173,61 @@ __device__ __forceinline__ void clear_counts(uint32_t* counts) {
 }
 __device__ __forceinline__ uint32_t key_of(int32_t token, int32_t V) { return token >= 0 && token < V ? (uint32_t)token : (uint32_t)V; }
 
-// Zeros into rows [V part / parts, V (part + 1) / parts) of dW, by the workgroups from `first` on; a wavefront a row.
+// Zeros into rows [V part / parts, V (part + 1) / parts) of dW, by the workgroups from `first` on; 2^lanes_log2 lanes a row.
 struct Fill {
   char* table;
   int64_t stride_bytes, row_bytes;
   int32_t V, part, parts, blocks;  // blocks: 0 for none
+  int32_t lanes_log2;
 };
-__device__ __forceinline__ void zero_row(const Fill& f, int64_t r, int lane) {
+typedef uint32_t u32x4_line __attribute__((ext_vector_type(4)));
+// A row by the lanes sub = 0 .. of it.  A wavefront on a row stores whole lines past the caches, and leaves in them what the row's
+// ends share with its neighbours, until those are written (23000 rows of 8224 bytes: 39 us
+// past the caches altogether, 30).  Lanes for several short rows: half a million of 16 bytes, 51 -> 23 us a call.
+__device__ __forceinline__ void zero_row(const Fill& f, int64_t r, int sub) {
   char* row = f.table + r * f.stride_bytes;
-  int64_t b = lane * 16;
-  for (; b + 16 <= f.row_bytes; b += 1024) __builtin_nontemporal_store(u32x4_any{0, 0, 0, 0}, (u32x4_any*)(row + b));
-  // at most one piece of the row's end is left, to one lane; rows are whole elements of 2 or 4 bytes
-  if (b < f.row_bytes)
-    for (; b < f.row_bytes; b += 2) *(uint16_t*)(row + b) = 0;
+  int64_t from = 0;  // rows are whole elements of 2 or 4 bytes
+  if (f.lanes_log2 == 6) {
+    const int head = (int)(-(uintptr_t)row & 127);
+    if (2 * sub < head) *(uint16_t*)(row + 2 * sub) = 0;
+    from = head + ((f.row_bytes - head) & ~(int64_t)127);
+    for (int64_t b = head + sub * 16; b < from; b += 1024) __builtin_nontemporal_store(u32x4_line{0, 0, 0, 0}, (u32x4_line*)(row + b));
+  }
+  for (from += sub * 16; from + 16 <= f.row_bytes; from += 16 << f.lanes_log2) *(u32x4_any*)(row + from) = u32x4_any{0, 0, 0, 0};
+  // at most one piece of the row's end is left, to one lane
+  if (from < f.row_bytes)
+    for (; from < f.row_bytes; from += 2) *(uint16_t*)(row + from) = 0;
+}
+// lanes for a row of so many bytes: a wavefront where it has a whole line at least, wherever it starts
+int fill_lanes_log2(int64_t row_bytes) {
+  int l = 0;
+  while (l < 6 && (16 << l) < row_bytes) ++l;
+  return l;
 }
 __device__ __forceinline__ void fill_rows(const Fill& f, int block) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, sub = lane & ((1 << f.lanes_log2) - 1);
   const int64_t waves = (int64_t)f.blocks * kSortWaves, wave = (int64_t)block * kSortWaves + (threadIdx.x >> 6);
   const int64_t from = (int64_t)f.V * f.part / f.parts, to = (int64_t)f.V * (f.part + 1) / f.parts;
-  for (int64_t r = from + wave; r < to; r += waves) zero_row(f, r, lane);
+  for (int64_t r = from + (wave << (6 - f.lanes_log2)) + (lane >> f.lanes_log2); r < to; r += waves << (6 - f.lanes_log2)) zero_row(f, r, sub);
 }
 
 // The one-launch sort: workgroup w owns the ids [w bins, (w + 1) bins), and each of its wavefronts reads a stretch of the tokens,
 // counts those of each of its ids and of all smaller ones and lists the former in LDS, in order.  A wavefront then ranks 64 listed
 // ones at a time among those of the same id by ballots over the bits; the counts of the wavefronts in front and of the smaller ids
 // make up the rest of a place.  Bound by the instructions of the scan, some 13 a token of a lane.  Where a few ids have so many of
-// the tokens that a wavefront's part of the list is too short, all are read again, for kGroupList places of the whole list at a time.
+// the tokens that a wavefront's part of the list is too short, all are read twice again, to count each wavefront's tokens of each id
+// and to place them (131072 tokens, half of them one id: 261 us with the list in pieces, a reading for each, 95).
 // 65536 tokens, 32000 ids, us: tiles of 16384 tokens listed one after the other in a second reading 28, the whole stretch in a second
 // reading 24, in the first 21; 8192 tokens, 128256 ids: 26.8 with one workgroup that sorts nine bits at a time in LDS, 7.5.
 struct GroupLds {
   uint16_t counts[kGroupBins * kSortWaves];  // of the listed tokens, [id][wavefront]
-  uint16_t id[kGroupList], rank[kGroupList];
-  uint32_t pos[kGroupList];
+  union {
+    struct {
+      uint16_t id[kGroupList], rank[kGroupList];
+      uint32_t pos[kGroupList];
+    };
+    uint32_t next[kGroupBins * kSortWaves];  // without a list: a wavefront's next place of each id, [id][wavefront]
+  };
   uint32_t place[kGroupBins];                // counts, then the next place, of each id
   uint32_t sums[kSortWaves], below[kSortWaves], mine[kSortWaves];
   uint64_t has[kSortWaves];                  // ids with a token, a bit each
@@ -225,9 +248,20 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
   const int lo = (int)((int64_t)blockIdx.x * bins), own_ids = min(bins, V - lo);
   const uint64_t in_front = ((uint64_t)1 << lane) - 1;
   auto of_mine = [&](int t) { return (uint32_t)(t - lo) < (uint32_t)own_ids; };  // tokens that are none are below 0 or from V on
-  // A lane's four tokens from position pos on into the list: the wavefront's first one goes to place at; nothing to place `limit` or
-  // behind it, nor to one below 0.  Returns how many of the wavefront's tokens there are.
-  auto list = [&](const i32x4_any& t, int pos, uint32_t at, uint32_t limit, auto each) {
+  // Counts of this range's ids.  The first lane's id is counted once for all that have it: frequent ones do not queue up in LDS.
+  // Whole numbers, the order does not matter.
+  auto count = [&](const i32x4_any& t, const uint64_t (&b)[4], uint32_t* counts, int step) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (b[j] == 0) continue;
+      const int lead = __builtin_ctzll(b[j]), id = __builtin_amdgcn_readlane(t[j], lead);
+      const uint32_t same = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(t[j] == id));
+      if (of_mine(t[j]) && (t[j] != id || lane == lead)) atomicAdd(&counts[(t[j] - lo) * step], t[j] == id ? same : 1u);
+    }
+  };
+  // A lane's four tokens from position pos on into the wavefront's part of the list behind its first `at`.  Returns how many of the
+  // wavefront's tokens there are.
+  auto list = [&](const i32x4_any& t, int pos, uint32_t at) {
     uint64_t b[4];
     uint32_t n = 0;
 #pragma unroll
@@ -236,16 +270,16 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
       n += (uint32_t)__popcll(b[j]);
     }
     if (n == 0) return 0u;
+    count(t, b, l.place, 1);
     uint32_t to = at;  // of this lane's first: the lanes in front, four tokens each
 #pragma unroll
     for (int j = 0; j < 4; ++j) to += (uint32_t)__popcll(b[j] & in_front);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (of_mine(t[j])) {
-        each((uint32_t)(t[j] - lo));
-        if (to < limit) {
-          l.id[to] = (uint16_t)(t[j] - lo);
-          l.pos[to] = (uint32_t)(pos + j);
+        if (to < kWaveList) {
+          l.id[wave * kWaveList + to] = (uint16_t)(t[j] - lo);
+          l.pos[wave * kWaveList + to] = (uint32_t)(pos + j);
         }
         ++to;
       }
@@ -266,11 +300,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
         below += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)t[k][j] < (uint32_t)lo));
       }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      mine += list(t[k], i0 + k * 256 + lane * 4, wave * kWaveList + mine, (wave + 1) * kWaveList, [&](uint32_t id) {
-        atomicAdd(&l.place[id], 1u);  // whole numbers: the order does not matter
-      });
-    }
+    for (int k = 0; k < 4; ++k) mine += list(t[k], i0 + k * 256 + lane * 4, mine);
   }
   if (lane == 0) {
     l.below[wave] = below;
@@ -280,52 +310,39 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
   const uint32_t of_id = l.place[tid];
   const uint64_t has = __builtin_amdgcn_ballot_w64(of_id != 0);
   if (lane == 0) l.has[wave] = has;
-  // places in front of this range; this wavefront's first place in the whole list; its length; the longest part
-  uint32_t base = 0, list_at = 0, all = 0, longest = 0;
+  // places in front of this range; its tokens; the longest part of the list
+  uint32_t base = 0, all = 0, longest = 0;
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) {
     base += l.below[w];
-    list_at += w < wave ? l.mine[w] : 0;
     all += l.mine[w];
     longest = max(longest, l.mine[w]);
   }
   const uint32_t place = base + before_me(of_id, l.sums);
   __syncthreads();
   l.place[tid] = place;
-  all = __builtin_amdgcn_readfirstlane(all);
-  list_at = __builtin_amdgcn_readfirstlane(list_at);
-  const bool again = __builtin_amdgcn_readfirstlane(longest) > kWaveList;  // the list is made in pieces of the whole
-  for (uint32_t from = 0; from < all; from += again ? kGroupList : all) {
-    if (from > 0) __syncthreads();  // what was listed before has its places
-    for (int i = tid; i < kGroupBins * kSortWaves / 8; i += kSortThreads) ((u32x4_any*)l.counts)[i] = u32x4_any{0, 0, 0, 0};
-    if (again && mine > 0 && list_at < from + kGroupList && list_at + mine > from) {
-      uint32_t at = list_at - from;  // may be below 0: such places are compared as large ones
-      for (int i0 = begin; i0 < end; i0 += 1024) {
-        i32x4_any t[4];
+  // which of the tokens (id d; a lane each) have the same id, and how many of them are in front
+  auto of_same_id = [&](bool is, uint32_t d) {
+    uint64_t same = __builtin_amdgcn_ballot_w64(is);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, end, i0 + k * 256 + lane * 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) at += list(t[k], i0 + k * 256 + lane * 4, at, kGroupList, [](uint32_t) {});
-      }
+    for (int b = 0; b < 10; ++b) {
+      const bool one = (d >> b) & 1;
+      const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
+      same &= one ? ones : ~ones;
     }
+    return same;
+  };
+  // LDS operations of a wavefront are in order: all read a count before the first token of each id raises it
+  if (__builtin_amdgcn_readfirstlane(longest) <= kWaveList) {
+    for (int i = tid; i < kGroupBins * kSortWaves / 8; i += kSortThreads) ((u32x4_any*)l.counts)[i] = u32x4_any{0, 0, 0, 0};
     __syncthreads();
-    // the listed ones that this wavefront places: entries first, first + 64, ... below n
-    const uint32_t n = again ? min(all - from, (uint32_t)kGroupList) : wave * kWaveList + mine;
-    const int rounds = again ? (int)((n + kSortThreads - 1) / kSortThreads) : (int)(mine + 63) / 64;
-    const int first = (again ? wave * rounds * 64 : wave * kWaveList) + lane;
+    const uint32_t first = wave * kWaveList + lane, end_of_list = wave * kWaveList + mine;
     volatile uint16_t* const counts = l.counts;
-    for (int e = 0; e < rounds; ++e) {
-      const uint32_t i = first + e * 64;
-      const bool is = i < n;
+    for (uint32_t i = first; i - lane < end_of_list; i += 64) {
+      const bool is = i < end_of_list;
       const uint32_t d = is ? l.id[i] : 0;
-      uint64_t same = __builtin_amdgcn_ballot_w64(is);
-#pragma unroll
-      for (int b = 0; b < 10; ++b) {
-        const bool one = (d >> b) & 1;
-        const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
-        same &= one ? ones : ~ones;
-      }
-      if (is) {  // LDS operations of a wavefront are in order: all read the count before the first of each id raises it
+      const uint64_t same = of_same_id(is, d);
+      if (is) {
         const uint32_t before = counts[d * kSortWaves + wave], r = (uint32_t)__popcll(same & in_front);
         __builtin_amdgcn_wave_barrier();
         if (r == 0) counts[d * kSortWaves + wave] = (uint16_t)(before + (uint32_t)__popcll(same));
@@ -334,9 +351,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
       }
     }
     __syncthreads();
-    for (int e = 0; e < rounds; ++e) {
-      const uint32_t i = first + e * 64;
-      if (i >= n) break;
+    for (uint32_t i = first; i < end_of_list; i += 64) {
       const uint32_t d = l.id[i];
       uint32_t to = l.place[d] + l.rank[i];
 #pragma unroll
@@ -344,19 +359,61 @@ __global__ __launch_bounds__(kSortThreads) void embed_group_kernel(const int32_t
       keys[to] = (uint32_t)lo + d;
       order[to] = l.pos[i];
     }
-    if (again && from + kGroupList < all) {
-      __syncthreads();
-      for (int e = 0; e < rounds; ++e) {
-        const uint32_t i = first + e * 64;
-        if (i < n) atomicAdd(&l.place[l.id[i]], 1u);
+  } else {
+    __syncthreads();  // the places are there, and nothing reads the list any more
+    for (int i = tid; i < kGroupBins * kSortWaves / 4; i += kSortThreads) ((u32x4_any*)l.next)[i] = u32x4_any{0, 0, 0, 0};
+    __syncthreads();
+    for (int i0 = begin; i0 < end; i0 += 1024) {
+      i32x4_any t[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] = load_tokens(tokens, end, i0 + k * 256 + lane * 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint64_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = __builtin_amdgcn_ballot_w64(of_mine(t[k][j]));
+        count(t[k], b, l.next + wave, kSortWaves);
+      }
+    }
+    __syncthreads();
+    uint32_t at = place;  // of this thread's id
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = l.next[tid * kSortWaves + w];
+      l.next[tid * kSortWaves + w] = at;
+      at += c;
+    }
+    __syncthreads();
+    volatile uint32_t* const next = l.next;
+    for (int i0 = begin; i0 < end; i0 += 512) {
+      int t[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = i0 + k * 64 + lane < end ? tokens[i0 + k * 64 + lane] : -1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool is = of_mine(t[k]);
+        const uint64_t any = __builtin_amdgcn_ballot_w64(is);
+        if (any == 0) continue;
+        const int lead = __builtin_amdgcn_readlane(t[k], __builtin_ctzll(any));
+        uint64_t same = __builtin_amdgcn_ballot_w64(t[k] == lead);
+        const uint32_t d = is ? (uint32_t)(t[k] - lo) : 0;
+        if (same != any) same = of_same_id(is, d);
+        if (is) {
+          const uint32_t before = next[d * kSortWaves + wave], r = (uint32_t)__popcll(same & in_front);
+          __builtin_amdgcn_wave_barrier();
+          if (r == 0) next[d * kSortWaves + wave] = before + (uint32_t)__popcll(same);
+          __builtin_amdgcn_wave_barrier();
+          keys[before + r] = (uint32_t)lo + d;
+          order[before + r] = (uint32_t)(i0 + k * 64 + lane);
+        }
       }
     }
   }
   if ((int)blockIdx.x == (int)gridDim.x - 1)  // behind the last token: none
     for (int64_t i = (int64_t)base + all + tid; i < T; i += kSortThreads) keys[i] = (uint32_t)V;
   if (fill.blocks) {
-    for (int r = wave; r < own_ids; r += kSortWaves)
-      if (!(l.has[r >> 6] >> (r & 63) & 1)) zero_row(fill, lo + r, lane);
+    const int shift = 6 - fill.lanes_log2, sub = lane & ((1 << fill.lanes_log2) - 1);
+    for (int r = (wave << shift) + (lane >> fill.lanes_log2); r < own_ids; r += kSortWaves << shift)
+      if (!(l.has[r >> 6] >> (r & 63) & 1)) zero_row(fill, (int64_t)lo + r, sub);
   }
 }
 
@@ -542,41 +599,87 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(EmbedParams p, S
   end_run(goes_on);
 }
 
-// The run that begins in chunk c and goes beyond it: its parts, in the chunks' order.
+// The runs that go beyond their chunk: the parts in the chunks' order.
+//
+// A run over fewer than kLongRun chunks behind its first: a wavefront has 64 vectors of it, and looks from every chunk whether one
+// begins there.  A longer one (a filler's id may have half of the tokens) covers some chunk whose number is a multiple of kLongRun, and
+// is found from the first of these: a workgroup has 16 vectors of it and sums 16 stretches of the parts side by side, in order in
+// the end.  131072 tokens of width 4096, half of them one id: 296 us with a wavefront for it, 35.
+constexpr int kLongRun = 64, kLongStretches = 16, kLongVectors = 16;
 template <int TABLE, int VEC, bool ADD>
-__global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, Sorted s, typename RowType<TABLE>::T* d_table, int wpr) {
-  const int64_t w = (int64_t)blockIdx.x * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+__device__ __forceinline__ void add_run(const EmbedParams& p, typename RowType<TABLE>::T* d_table, uint32_t k, const Span& at, const f32x8_row& acc,
+                                        const RawSpan<TABLE, VEC>& had) {
+  store_span<TABLE, VEC>(d_table + (int64_t)k * p.table_st, at, ADD ? had.widen() + acc * p.scale : acc * p.scale);
+}
+// parts [from, to) of the run that begins in chunk c; part 0 is that chunk's end, the others are their chunks' beginnings
+template <int VEC>
+__device__ __forceinline__ f32x8_row sum_parts(const Sorted& s, int dim, int c, int col, int from, int to) {
+  constexpr int U = 16;
+  const float* part = s.part + (int64_t)c * 2 * dim + col;
+  f32x8_row acc = {};
+  for (int i = from; i < to; i += U) {
+    f32x8_row x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      x[u] = i + u < to ? load_span<HBP_F32, VEC>(part + (i + u == 0 ? (int64_t)dim : (int64_t)(i + u) * 2 * dim)) : f32x8_row{};
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc += x[u];
+  }
+  return acc;
+}
+template <int TABLE, int VEC, bool ADD>
+__global__ __launch_bounds__(kRowThreads) void embed_join_kernel(EmbedParams p, Sorted s, typename RowType<TABLE>::T* d_table, int wpr, int long_groups) {
+  __shared__ f32x8_row sums[kLongStretches][kLongVectors];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
+  if ((int)blockIdx.x < long_groups) {
+    const int per_run = (n_vec + kLongVectors - 1) / kLongVectors, here = (blockIdx.x / (unsigned)per_run + 1) * kLongRun;
+    const uint32_t k = s.keys[here * s.chunk];
+    if (k >= (uint32_t)p.V || s.keys[here * s.chunk - 1] != k) return;
+    // the chunk that it begins in: the nearest before this one whose first entry does not go on with it
+    const int b = here - 1 - lane;
+    const uint64_t begins = __builtin_amdgcn_ballot_w64(b == 0 || s.keys[b * s.chunk - 1] != k);
+    if (begins == 0) return;  // further away: another multiple's
+    const int c = here - 1 - __builtin_ctzll(begins);
+    int last = here, end = s.n_chunks;  // the last chunk that begins with it is in [last, end)
+    while (end - last > 1) {
+      const int step = (end - last + 63) / 64, at = last + (lane + 1) * step;
+      const int n = __popcll(__builtin_amdgcn_ballot_w64(at < end && s.keys[(at < end ? at : 0) * s.chunk] == k));
+      end = min(end, last + (n + 1) * step);
+      last += n * step;
+    }
+    const int n = last - c;
+    if (n < kLongRun) return;
+    const int v = (int)(blockIdx.x % (unsigned)per_run) * kLongVectors + (lane & (kLongVectors - 1)), stretch = wave * 4 + (lane >> 4);
+    const Span at = span_of<VEC>(min(v, n_vec - 1), p.dim);
+    const int per = (n + kLongStretches) / kLongStretches, from = stretch * per;  // of n + 1 parts
+    sums[stretch][lane & (kLongVectors - 1)] = sum_parts<VEC>(s, p.dim, c, at.col, from, min(from + per, n + 1));
+    __syncthreads();
+    if ((int)threadIdx.x >= kLongVectors || v >= n_vec) return;
+    RawSpan<TABLE, VEC> had;
+    if (ADD) had = RawSpan<TABLE, VEC>(d_table + (int64_t)k * p.table_st + at.col);
+    f32x8_row acc = sums[0][lane];
+#pragma unroll
+    for (int i = 1; i < kLongStretches; ++i) acc += sums[i][lane];
+    add_run<TABLE, VEC, ADD>(p, d_table, k, at, acc, had);
+    return;
+  }
+  const int64_t w = (int64_t)(blockIdx.x - long_groups) * (kRowThreads / 64) + wave;
   const int c = (int)(w / wpr);
   if (c + 1 >= s.n_chunks) return;  // nothing goes beyond the last one
   const int first = c * s.chunk, next = first + s.chunk;
   const uint32_t k = s.keys[next - 1];
   if (k >= (uint32_t)p.V || s.keys[next] != k) return;
   if (s.keys[first] == k && first > 0 && s.keys[first - 1] == k) return;  // it began earlier
-  int n = 0;  // chunks behind this one that begin with the run
-  for (int lane = threadIdx.x & 63;; lane += 64) {
-    const int64_t at = (int64_t)(c + 1 + lane) * s.chunk;
-    const uint64_t in = __builtin_amdgcn_ballot_w64(at < p.T && s.keys[at < p.T ? at : 0] == k);
-    n += __popcll(in);
-    if (~in) break;
-  }
-  const int v = (int)(w - (int64_t)c * wpr) * 64 + (threadIdx.x & 63);
-  const int n_vec = VEC == 8 ? (p.dim + 7) / 8 : p.dim;
+  const int b = c + 1 + lane;
+  const uint64_t in = __builtin_amdgcn_ballot_w64(b < s.n_chunks && s.keys[(b < s.n_chunks ? b : 0) * s.chunk] == k);
+  const int n = __popcll(in);  // chunks behind this one that begin with the run
+  if (n == kLongRun) return;
+  const int v = (int)(w - (int64_t)c * wpr) * 64 + lane;
   if (v >= n_vec) return;
   const Span at = span_of<VEC>(v, p.dim);
-  auto* row = d_table + (int64_t)k * p.table_st;
   RawSpan<TABLE, VEC> had;
-  if (ADD) had = RawSpan<TABLE, VEC>(row + at.col);
-  const float* part = s.part + (int64_t)c * 2 * p.dim + at.col;
-  f32x8_row acc = load_span<HBP_F32, VEC>(part + p.dim);
-  constexpr int U = 16;
-  for (int i = 1; i <= n; i += U) {
-    f32x8_row x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = i + u <= n ? load_span<HBP_F32, VEC>(part + (int64_t)(i + u) * 2 * p.dim) : f32x8_row{};
-#pragma unroll
-    for (int u = 0; u < U; ++u) acc += x[u];
-  }
-  store_span<TABLE, VEC>(row, at, ADD ? had.widen() + acc * p.scale : acc * p.scale);
+  if (ADD) had = RawSpan<TABLE, VEC>(d_table + (int64_t)k * p.table_st + at.col);
+  add_run<TABLE, VEC, ADD>(p, d_table, k, at, sum_parts<VEC>(s, p.dim, c, at.col, 0, n + 1), had);
 }
 
 template <int TABLE, int ROW, int VEC>
@@ -601,7 +704,9 @@ int sums(const EmbedParams& p, const Sorted& srt, const void* d_out, void* d_tab
   hipLaunchKernelGGL((embed_sum_kernel<ROW, TABLE, VEC, ADD, 8>), grid, dim3(kRowThreads), 0, s, p, srt, (const typename RowType<ROW>::T*)d_out, w, wpr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || srt.n_chunks < 2) return (int)e;
-  hipLaunchKernelGGL((embed_join_kernel<TABLE, VEC, ADD>), grid, dim3(kRowThreads), 0, s, p, srt, w, wpr);
+  const int64_t long_groups = (int64_t)((srt.n_chunks - 1) / kLongRun) * ((n_vectors(p.dim) + kLongVectors - 1) / kLongVectors);
+  if (long_groups + groups > 0x7fffffff) return (int)hipErrorInvalidValue;
+  hipLaunchKernelGGL((embed_join_kernel<TABLE, VEC, ADD>), dim3((unsigned)(long_groups + groups)), dim3(kRowThreads), 0, s, p, srt, w, wpr, (int)long_groups);
   return (int)hipGetLastError();
 }
 template <int ROW, int TABLE>
@@ -655,7 +760,7 @@ int launch_embed_bwd(const EmbedParams& p, int table_type, int row_type, const v
   const int es = table_type == HBP_BF16 ? 2 : 4, bits = key_bits(p.V);
   uint32_t* keys[2] = {(uint32_t*)(ws + l.keys_off[0]), (uint32_t*)(ws + l.keys_off[1])};
   uint32_t* order[2] = {(uint32_t*)(ws + l.order_off[0]), (uint32_t*)(ws + l.order_off[1])};
-  Fill fill{(char*)d_table, p.table_st * es, (int64_t)p.dim * es, p.V, 0, 1, 0};
+  Fill fill{(char*)d_table, p.table_st * es, (int64_t)p.dim * es, p.V, 0, 1, 0, fill_lanes_log2((int64_t)p.dim * es)};
   // workgroups of 16 wavefronts, a row a wavefront at a time
   const int fill_blocks = accumulate ? 0 : (int)((p.V + kSortWaves - 1) / kSortWaves < 2048 ? (p.V + kSortWaves - 1) / kSortWaves : 2048);
   int at = 0;
