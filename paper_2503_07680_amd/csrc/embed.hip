@@ -36,11 +36,15 @@ int log2_threads_per_row(int n_vec) {  // 64 to 256: a wavefront is always on on
   return n_vec > 128 ? 8 : n_vec > 64 ? 7 : 6;
 }
 int waves_per_row(int n_vec) { return (n_vec + 63) / 64; }
-// Ids of a workgroup of the one-launch sort; 0: that reads too much (a quarter of a million tokens for each of 256 workgroups
-// or more), the radix sort is taken.
+// Ids of a workgroup of the one-launch sort; 0: the radix sort is taken, where every workgroup would read very many tokens, or there
+// would be very many of them (a compute unit holds one).  Whole calls on narrow rows, us, one launch / radix sort, ids of frequencies
+// 1/n, or (equal / half of the tokens one id): 1000 tokens 17 / 28; 32768: 33 / 46; 65536: 44 / 50 (30 / 47; 73 / 54);
+// 131072: 69 / 59 (43 / 56; 125 / 67); 196608: 166 / 68; a million ids: 1000 29 / 37, 32768 49 / 63, 131072 80 / 67; two million: 42 /
+// 37, 51 / 52 with 8192, 71 / 62 with 32768; four million: 65 / 38, 82 / 52 with 8192.
 int group_bins(int32_t T, int32_t V) {
   const int bins = V <= 256 * kGroupBins ? (V + 255) / 256 : kGroupBins;
-  return (int64_t)T * ((V + (int64_t)bins - 1) / bins) <= ((int64_t)1 << 26) ? bins : 0;
+  const int64_t groups = (V + (int64_t)bins - 1) / bins;
+  return T <= 65536 && groups <= 2048 && T * groups <= ((int64_t)1 << 25) ? bins : 0;
 }
 int n_vectors(int dim) { return dim >= 8 ? (dim + 7) / 8 : dim; }
 int key_bits(int32_t V) { return 32 - __builtin_clz((uint32_t)V); }  // ids 0 .. V - 1, and V for "no token"
@@ -216,7 +220,7 @@ __device__ __forceinline__ void fill_rows(const Fill& f, int block) {
 // ones at a time among those of the same id by ballots over the bits; the counts of the wavefronts in front and of the smaller ids
 // make up the rest of a place.  Bound by the instructions of the scan, some 13 a token of a lane.  Where a few ids have so many of
 // the tokens that a wavefront's part of the list is too short, all are read twice again, to count each wavefront's tokens of each id
-// and to place them (131072 tokens, half of them one id: 261 us with the list in pieces, a reading for each, 95).
+// and to place them (16384 tokens of width 2048, half of them one id: a call of 90 us, half of that the joins below, is 48).
 // 65536 tokens, 32000 ids, us: tiles of 16384 tokens listed one after the other in a second reading 28, the whole stretch in a second
 // reading 24, in the first 21; 8192 tokens, 128256 ids: 26.8 with one workgroup that sorts nine bits at a time in LDS, 7.5.
 struct GroupLds {

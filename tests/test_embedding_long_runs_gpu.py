@@ -71,3 +71,19 @@ def test_rows_without_tokens_are_zeroed_and_nothing_else(dim, table_type):
         assert bool((view[t.long().cuda()] != 0).any())
         view.fill_(7.0)
         assert bool((base == 7.0).all())
+
+
+@pytest.mark.parametrize("runs", [[12288, 1, 700], [20000, 30000, 4000, 9], [9000] * 7, [800, 13000, 1, 1, 600, 65, 30000], [65535, 1], [13000]],
+                         ids=lambda r: "-".join(map(str, r[:5])))
+@pytest.mark.parametrize("ordered", [False, True])
+def test_frequent_ids_beside_each_other(runs, ordered):
+    """All of them in one workgroup's range of ids, mixed, or each in a stretch of its own."""
+    T, vocab, dim = sum(runs), 300000, 16
+    g = torch.Generator().manual_seed(T)
+    t = torch.repeat_interleave(torch.arange(len(runs)) * 3 + 200000, torch.tensor(runs)).to(torch.int32)
+    t = t.flip(0) if ordered else t[torch.randperm(T, generator=g)]
+    d = torch.randint(-8, 9, (T, dim), generator=g).to(F32)
+    e = module()(T, vocab, dim, 1.0, F32, F32)
+    got = e.backward(d.cuda(), t.cuda(), torch.empty(vocab, dim, device="cuda"))
+    want = torch.zeros(vocab, dim, dtype=torch.float64).index_add_(0, t.long(), d.double())
+    assert torch.equal(got.cpu().double(), want)            # whole numbers below 2^24: exact
