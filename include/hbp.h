@@ -419,6 +419,8 @@ typedef struct {
   float softmax_scale; /* <= 0: 1/sqrt(d_qk) */
   int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h;
   int64_t v_stride_t, v_stride_h, o_stride_t, o_stride_h;
+  int32_t longest_keys; /* keys of the longest sample that has queries, 0: unknown (the mean is taken).  It goes into the workspace
+                         * of the forward and how it deals out the keys; one that does not hold costs time, not results. */
 } hbp_cross_desc;
 
 /* Rows per tile that the kernels expect from hbp_cross_plan: which = HBP_FWD: query tokens of a query tile (256 divided by the

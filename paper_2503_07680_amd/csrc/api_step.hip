@@ -99,7 +99,7 @@ hbp_status check_cross(const hbp_cross_desc* d) {
   if (!d) return HBP_ERR_INVALID_ARG;
   if (d->total_queries < 0 || d->total_keys < 0 || d->n_samples < 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->d_qk <= 0 || d->d_v <= 0)
     return HBP_ERR_INVALID_ARG;
-  if (!std::isfinite(d->softmax_scale)) return HBP_ERR_INVALID_ARG;
+  if (!std::isfinite(d->softmax_scale) || d->longest_keys < 0) return HBP_ERR_INVALID_ARG;
   if (d->n_q_heads % d->n_kv_heads) return HBP_ERR_SHAPE;
   if (!((d->d_qk == 64 && d->d_v == 64) || (d->d_qk == 128 && d->d_v == 128) || (d->d_qk == 192 && d->d_v == 128))) return HBP_ERR_UNSUPPORTED;
   const hbp::CrossStrides s = hbp::cross_strides(*d);
@@ -168,6 +168,7 @@ extern "C" hbp_status hbp_cross_attn_fwd(const hbp_cross_desc* desc, const void*
   p.v_st = s.v_t; p.v_sh = s.v_h; p.o_st = s.o_t; p.o_sh = s.o_h;
   p.scale_log2 = scale_of(desc) * kLog2e;
   p.parts = lay.parts;
+  p.part_keys = lay.part_keys;
   p.o_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.o_off);
   p.ml_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.ml_off);
   return hbp::launch_cross_fwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;

@@ -245,6 +245,9 @@ struct Fold {
   }
 };
 
+// Keys of a part, where a sample's n keys are dealt out in `parts` at most, of `least` at least; whole key tiles.
+__device__ __forceinline__ int keys_of_a_part(int n, int parts, int least) { return (max((n + parts - 1) / parts, least) + 63) / 64 * 64; }
+
 // Tile copy with the lane-dependent part (LDS row, swizzled chunk) packed once per kernel.  Rows
 // >= rows_valid re-read the last valid row (never out of bounds; the caller masks their products).
 template <int D, int ROWS, int NW = 4>
@@ -789,7 +792,7 @@ struct FwdParams {
   // the number of folded groups that read one kv head, and a "head" of an item is such a group.
   const int32_t* cu_kv;
   int32_t Tk, fold_log2;
-  int32_t parts;           // a sample's keys are dealt out in so many; from two on:
+  int32_t part_keys, parts;  // a sample's keys are dealt out in so many parts at most, of part_keys at least; from two on:
   float *o_part, *ml_part; // [part][folded group][token][F] of [d_v], and of {reference, row sum}
 };
 

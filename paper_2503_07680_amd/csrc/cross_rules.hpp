@@ -66,28 +66,44 @@ inline CrossTiles cross_tiles(const hbp_cross_desc& d) {
 //               256 queries, 8000 keys, 32/8 heads: 131 -> 48.4 (45.3); 1308, 16859 keys, 8/1: 269 -> 113 (98.7)
 //               517, 12494 keys, 64/8: 260 in one part (231 in three); 16 samples of 100 queries, 300 keys: 12 to 41 in one part,
 //               14 to 85 in two
-inline int cross_fwd_parts(const hbp_cross_desc& d) {
-  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return 1;
+//
+// The mean sample's parts are long for one that is much longer.  Where that one's would be more than 32 tiles, and 1.5 times a workgroup's
+// fair share of all tiles (three times, if there was one part for all), the share is the length of a part: the longest sample has as
+// many as it takes, the others fewer, and workgroups without keys end at once.  By the mean -> here, one token each:
+//   50000 keys and 31 of 200, 32/8 heads of 128: 238 -> 76; 24 heads: 907 -> 193; 127 of 200, 32/8: 888 -> 222, 8/1: 237 -> 85
+//   lengths log-normal, a spread of .8: 32 samples of 1500, 16 heads of 192: 204 -> 170, 32/8: 61 -> 57; 300 of 700, 8/1: 64 -> 54
+//   100 queries each, 20000 keys and 15 of 300, 32/8: 316 -> 112.  Below these lines it loses: parts of 12 to 22 tiles, 5 to 39 %
+struct CrossFwdParts {
+  int parts, keys;  // at most, for one sample; keys of a part at least
+};
+inline CrossFwdParts cross_fwd_parts(const hbp_cross_desc& d) {
+  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return {1, 0};
   const CrossTiles t = cross_tiles(d);
-  int64_t parts, most;
-  if (t.rows <= 32) {
-    parts = 768 / t.items;
-    most = t.key_tiles / 3 < 32 ? t.key_tiles / 3 : 32;
-  } else {
-    parts = 384 / (t.items * ((t.rows + 127) / 128));
-    most = t.key_tiles < 16 ? 1 : t.key_tiles / 6 < 16 ? t.key_tiles / 6 : 16;
-  }
+  const bool few = t.rows <= 32;
+  const int64_t groups = few ? 768 : 384, items = few ? t.items : t.items * ((t.rows + 127) / 128);
+  const int64_t least = few ? 3 : 6, most = few ? 32 : 16, begin = few ? 6 : 16;  // tiles of a part; parts; tiles below which there is one
+  int64_t parts = groups / items;
+  if (parts > t.key_tiles / least) parts = t.key_tiles / least;
   if (parts > most) parts = most;
-  return (int)(parts < 1 ? 1 : parts);
+  if (parts < 1 || t.key_tiles < begin) parts = 1;
+  const int64_t longest = ((int64_t)(d.longest_keys < d.total_keys ? d.longest_keys : d.total_keys) + 63) / 64;
+  int64_t share = (items * t.key_tiles + groups - 1) / groups;
+  if (share < least) share = least;
+  const int64_t part = longest / parts;
+  if (part <= 32 || 2 * part <= (parts > 1 ? 3 : 6) * share) return {(int)parts, 0};
+  parts = (longest + share - 1) / share;
+  return {(int)(parts > most ? most : parts), (int)(share * 64)};
 }
 struct CrossFwdLayout {
   size_t o_off, ml_off, total;
-  int parts;
+  int parts, part_keys;
 };
 inline CrossFwdLayout cross_fwd_layout(const hbp_cross_desc& d) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   CrossFwdLayout l;
-  l.parts = cross_fwd_parts(d);
+  const CrossFwdParts parts = cross_fwd_parts(d);
+  l.parts = parts.parts;
+  l.part_keys = parts.keys;
   const size_t rows = l.parts > 1 ? (size_t)l.parts * d.n_q_heads * d.total_queries : 0;
   l.o_off = 0;
   l.ml_off = up(rows * d.d_v * 4);

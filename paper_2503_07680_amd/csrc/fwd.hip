@@ -407,8 +407,10 @@ __device__ __forceinline__ void fwd_items() {
              tl.row_end - tl.row_begin <= (BM << halves) >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
              BM * half < (tl.row_end - tl.row_begin) << p.fold_log2;
         if (ok && p.parts > 1) {  // this workgroup's part of the keys
-          const int per = ((ks1 - ks0 + p.parts - 1) / p.parts + BN - 1) / BN * BN, from = min((int64_t)per * blockIdx.y, (int64_t)(ks1 - ks0));
-          ks1 = min(ks1 - ks0 - from, per) + ks0 + from;
+          static_assert(BN == 64, "a part is whole key tiles");
+          const int n = ks1 - ks0, per = keys_of_a_part(n, p.parts, p.part_keys), from = min((int64_t)per * blockIdx.y, (int64_t)n);
+          ok = from < n || blockIdx.y == 0;
+          ks1 = min(n - from, per) + ks0 + from;
           ks0 += from;
         }
       }
@@ -690,7 +692,7 @@ __global__ __launch_bounds__(kThreads * TP, 2 / TP) void cross_forward_kernel(co
   fwd_items<DQK, DV, 1, TP, true, true>();
 }
 
-// O and LSE of a tile's rows from their parts: with m the largest of the references m_i, O = sum 2^(m_i - m) O_i / l and
+// O and LSE of a tile's rows from the parts that its sample has: with m the largest of the references m_i, O = sum 2^(m_i - m) O_i / l and
 // LSE = (m + log2 l) ln 2, l = sum 2^(m_i - m) l_i.  DV / 4 lanes a row; bound by reading the parts once.  Grid: folded groups,
 // shares of the rows, tiles.
 template <int DV>
@@ -704,22 +706,23 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p)
         tl.row_end - tl.row_begin <= 256 >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk))
     return;
   const int n_rows = (tl.row_end - tl.row_begin) << p.fold_log2, x = threadIdx.x % LPR;
+  const int per = max(keys_of_a_part(ks1 - ks0, p.parts, p.part_keys), 64), parts = max((int)(((int64_t)ks1 - ks0 + per - 1) / per), 1);
   const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
   for (int f = blockIdx.y * (kThreads / LPR) + threadIdx.x / LPR; f < n_rows; f += gridDim.y * (kThreads / LPR)) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    for (int at = 0; at < p.parts; at += 4) {  // four parts' loads under way
+    for (int at = 0; at < parts; at += 4) {  // four parts' loads under way
       f32x2 ml[4];
       f32x4 o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t r = min(at + i, p.parts - 1) * rows + row0 + f;
+        const int64_t r = min(at + i, parts - 1) * rows + row0 + f;
         ml[i] = *(const f32x2*)(p.ml_part + 2 * r);
         o[i] = *(const f32x4*)(p.o_part + r * DV + 4 * x);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (at + i >= p.parts || ml[i][0] == -INFINITY) continue;  // a part without keys
+        if (at + i >= parts || ml[i][0] == -INFINITY) continue;  // a sample without keys
         const float top = fmaxf(m, ml[i][0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[i][0] - top);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + o[i][j] * b;

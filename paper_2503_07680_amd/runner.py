@@ -178,7 +178,8 @@ class PackedCrossAttention:
         self.Tq, self.Tk = int(sum(q_lengths)), int(sum(kv_lengths))
         self.desc = B.CrossDesc(total_queries=self.Tq, total_keys=self.Tk, n_samples=len(q_lengths),
                                 n_q_heads=self.Hq, n_kv_heads=self.Hkv, d_qk=self.d_qk, d_v=self.d_v,
-                                softmax_scale=float(softmax_scale))
+                                softmax_scale=float(softmax_scale),
+                                longest_keys=max((int(k) for q, k in zip(q_lengths, kv_lengths) if q), default=0))
         self.cu_q, self.cu_kv, q_tiles, self.pairs = B.hbp_cross_plan(
             q_lengths, kv_lengths, B.hbp_cross_tile_rows(self.desc, B.HBP_FWD), B.HBP_TILES_QUERY)
         _, _, kv_tiles, _ = B.hbp_cross_plan(

@@ -65,9 +65,13 @@ int main() {
     d.n_samples = size_up_to(20);
     d.n_kv_heads = 1 + (int32_t)(rnd() % 64);
     d.n_q_heads = d.n_kv_heads * (1 + (int32_t)(rnd() % 64));
+    d.longest_keys = rnd() % 2 ? 0 : size_up_to(31);
     d.d_qk = dims[round % 3][0];
     d.d_v = dims[round % 3][1];
-    const int fold = hbp::cross_fold_log2(d), parts = hbp::cross_parts(d), fwd = hbp::cross_fwd_parts(d), dq = hbp::cross_dq_parts(d);
+    const int fold = hbp::cross_fold_log2(d), parts = hbp::cross_parts(d), dq = hbp::cross_dq_parts(d);
+    const hbp::CrossFwdParts f_parts = hbp::cross_fwd_parts(d);
+    const int fwd = f_parts.parts;
+    CHECK(f_parts.keys >= 0 && f_parts.keys % 64 == 0 && (f_parts.keys == 0 || (d.longest_keys > 0 && fwd > 1 && f_parts.keys < INT_MAX - 4096)));
     CHECK(fold >= 0 && fold <= 5 && (d.n_q_heads / d.n_kv_heads) % (1 << fold) == 0);
     CHECK(parts >= 1 && parts <= 32 && fwd >= 1 && fwd <= 32 && dq >= 1 && dq <= 32);
     const hbp::CrossFwdLayout f = hbp::cross_fwd_layout(d);

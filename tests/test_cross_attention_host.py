@@ -128,3 +128,14 @@ def test_nothing_to_attend_or_to_ask():
     for kw in (dict(total_queries=0), dict(total_keys=0), dict(total_queries=0, total_keys=0, n_samples=0)):
         d = desc(**kw)
         assert H.hbp_cross_workspace_bytes(d, H.HBP_BWD) >= 0
+
+
+def test_the_longest_sample_goes_into_the_workspace():
+    """One sample of 50000 keys among short ones has parts of its own; a mild spread, an unknown one and a refused one do not."""
+    kw = dict(total_queries=32, total_keys=56200, n_samples=32, n_q_heads=24, n_kv_heads=24, d_qk=128, d_v=128)
+    need = {k: H.hbp_cross_workspace_bytes(H.CrossDesc(longest_keys=k, **kw), H.HBP_FWD) for k in (0, 1756, 3000, 50000)}
+    assert need[0] == need[1756] == need[3000] == 0 and need[50000] > 0
+    all_keys, more = (H.hbp_cross_workspace_bytes(H.CrossDesc(longest_keys=k, **kw), H.HBP_FWD) for k in (56200, 2 ** 31 - 1))
+    assert all_keys == more >= need[50000]
+    with pytest.raises(H.HbpError):
+        H.hbp_cross_workspace_bytes(H.CrossDesc(longest_keys=-1, **kw), H.HBP_FWD)
