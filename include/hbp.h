@@ -419,8 +419,11 @@ typedef struct {
   float softmax_scale; /* <= 0: 1/sqrt(d_qk) */
   int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h;
   int64_t v_stride_t, v_stride_h, o_stride_t, o_stride_h;
-  int32_t longest_keys; /* keys of the longest sample that has queries, 0: unknown (the mean is taken).  It goes into the workspace
-                         * of the forward and how it deals out the keys; one that does not hold costs time, not results. */
+  /* The most keys of a sample that has queries, the most query rows of one that has keys, and the sum over the samples of query rows
+   * times keys (hbp_cross_plan's pairs); 0: unknown, the means are taken.  They go into the workspaces and how the work is dealt
+   * out; values that do not hold cost time, not results. */
+  int32_t longest_keys, longest_queries;
+  int64_t pairs;
 } hbp_cross_desc;
 
 /* Rows per tile that the kernels expect from hbp_cross_plan: which = HBP_FWD: query tokens of a query tile (256 divided by the

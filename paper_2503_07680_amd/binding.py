@@ -81,7 +81,8 @@ class CrossDesc(ctypes.Structure):
                 ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
                 ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
                 ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
-                ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64), ("longest_keys", ctypes.c_int32)]
+                ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64), ("longest_keys", ctypes.c_int32), ("longest_queries", ctypes.c_int32),
+                ("pairs", ctypes.c_int64)]
 
 
 class EmbedDesc(ctypes.Structure):

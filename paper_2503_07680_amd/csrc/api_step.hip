@@ -99,7 +99,7 @@ hbp_status check_cross(const hbp_cross_desc* d) {
   if (!d) return HBP_ERR_INVALID_ARG;
   if (d->total_queries < 0 || d->total_keys < 0 || d->n_samples < 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->d_qk <= 0 || d->d_v <= 0)
     return HBP_ERR_INVALID_ARG;
-  if (!std::isfinite(d->softmax_scale) || d->longest_keys < 0) return HBP_ERR_INVALID_ARG;
+  if (!std::isfinite(d->softmax_scale) || d->longest_keys < 0 || d->longest_queries < 0 || d->pairs < 0) return HBP_ERR_INVALID_ARG;
   if (d->n_q_heads % d->n_kv_heads) return HBP_ERR_SHAPE;
   if (!((d->d_qk == 64 && d->d_v == 64) || (d->d_qk == 128 && d->d_v == 128) || (d->d_qk == 192 && d->d_v == 128))) return HBP_ERR_UNSUPPORTED;
   const hbp::CrossStrides s = hbp::cross_strides(*d);
@@ -227,7 +227,10 @@ extern "C" hbp_status hbp_cross_attn_bwd(const hbp_cross_desc* desc, const void*
   p.n_split_dq = 1;
   p.dk_part = reinterpret_cast<float*>(ws + lay.dk_part_off);
   p.dv_part = reinterpret_cast<float*>(ws + lay.dv_part_off);
+  p.part_steps = lay.part_steps;
+  p.dq_part_keys = lay.dq_part_keys;
   p.dq_parts = lay.dq_parts;
+  p.dq_first = lay.dq_first;
   p.dq_part = reinterpret_cast<float*>(ws + lay.dq_part_off);
   return hbp::launch_cross_bwd(desc->d_qk, desc->d_v, p, static_cast<hipStream_t>(stream)) ? HBP_ERR_DEVICE : HBP_OK;
 }

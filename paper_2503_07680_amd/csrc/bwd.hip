@@ -45,6 +45,12 @@ __device__ __forceinline__ StepRange part_of_steps(int64_t steps, int part, int 
   return {__builtin_amdgcn_readfirstlane((int)(steps * part / n_parts)), __builtin_amdgcn_readfirstlane((int)(steps * (part + 1) / n_parts))};
 }
 
+// The same where a part has `least` steps at least (0: no such bound): how many there are.
+__device__ __forceinline__ int parts_of_steps(int64_t steps, int most, int least) {
+  if (least == 0) return most;
+  return __builtin_amdgcn_readfirstlane((int)max((int64_t)1, min((int64_t)most, (steps + least - 1) / least)));
+}
+
 struct ProfAcc {
   uint32_t n_done = 0;
   uint64_t t_first = 0, t_last = 0, t_busy = 0, t0 = 0;
@@ -221,9 +227,10 @@ __device__ __forceinline__ void dq_items(int block) {
              tl.row_end - tl.row_begin <= 2 * BM >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk &&
              (HALVES == 2 || BM * row_half < (tl.row_end - tl.row_begin) << p.fold_log2);
         if (ok && p.dq_parts > 1) {
-          const int n = ks1 - ks0, per = ((n + p.dq_parts - 1) / p.dq_parts + BN - 1) / BN * BN, from = min((int64_t)per * key_part, (int64_t)n);
-          ks1 = ks0 + from + min(n - from, per);
-          ks0 += from;
+          const KeyParts of = key_parts(ks1 - ks0, p.dq_parts, p.dq_part_keys);
+          ok = key_part < of.n;
+          ks0 += ok ? of.keys * key_part : 0;
+          ks1 = min((int64_t)ks0 + of.keys, (int64_t)ks1);
         }
       }
     } else if (ok) {
@@ -492,7 +499,9 @@ __device__ __forceinline__ void dq_items(int block) {
       if (CROSS && nkt == 0) wait_async_loads();  // no tile has waited for the rows
       __syncthreads();  // the tiles are no longer read
       race_fence();
-      if (CROSS && p.dq_parts > 1) {
+      // read again: to hold it would cost copies of the accumulators in the loop
+      const int n_parts = CROSS ? key_parts(p.cu_kv[tl.sample + 1] - p.cu_kv[tl.sample], p.dq_parts, p.dq_part_keys).n : 1;
+      if (CROSS && n_parts > 1) {
         if (row_valid) {
           const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2;
           float* out = p.dq_part + (key_part * rows + (((int64_t)h * p.T + tl.row_begin) << p.fold_log2) + my_row) * DQK + 4 * hh;
@@ -639,7 +648,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
 
     hbp_tile tl;
     int s0, s1;
-    int qs0 = 0, qs1 = 0;
+    int qs0 = 0, qs1 = 0, n_parts = p.n_split;
     bool ok;
     if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx, p.cu_kv, p.cu, p.n_samples, lane, tl, s0, s1, qs0, qs1);
     else ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
@@ -647,6 +656,10 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
       if (ok) {
         ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
+        if (ok && p.part_steps > 0) {
+          n_parts = parts_of_steps((int64_t)((((qs1 - qs0) << p.fold_log2) + BQ - 1) / BQ) * g_item, p.n_split, p.part_steps);
+          ok = part < n_parts;
+        }
       }
     } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
@@ -663,7 +676,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
 
       const int qb_start = CROSS ? 0 : (k0_in / BQ) * BQ;
       const int nqb = (s_len - qb_start + BQ - 1) / BQ;
-      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, p.n_split) : StepRange{0, nqb * g_item};
+      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, n_parts) : StepRange{0, nqb * g_item};
       const int n_steps = range.to - range.from;
 
       // Step order: the query blocks from the LAST one of the sample down to the tile's own, and for each
@@ -999,6 +1012,7 @@ __device__ __forceinline__ void dkdv_items(int block, int n_resident) {
       }
 
       if (CROSS && n_steps == 0) wait_async_loads();  // no query rows: no step has waited for the rows of K and V
+      // CROSS: not by the item's number of parts, which would cost copies of the accumulators in the loop if it were held to here
       if (p.n_split == 1) {
         if (wave_active) {  // both through the wave's rows of K
           RowStage<DQK>::put(k_at, lane, dkt, -p.scale);
@@ -1155,7 +1169,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
 
     hbp_tile tl;
     int s0, s1;
-    int qs0 = 0, qs1 = 0;
+    int qs0 = 0, qs1 = 0, n_parts = p.n_split;
     bool ok;
     if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx, p.cu_kv, p.cu, p.n_samples, lane, tl, s0, s1, qs0, qs1);
     else ok = load_tile(p.tiles, tile_idx, p.cu, p.n_samples, lane, tl, s0, s1);
@@ -1163,6 +1177,10 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
       if (ok) {
         ok = s0 >= 0 && s1 <= p.Tk && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
              tl.row_end - tl.row_begin <= BN && 0 <= qs0 && qs0 <= qs1 && qs1 <= p.T;
+        if (ok && p.part_steps > 0) {
+          n_parts = parts_of_steps((int64_t)((((qs1 - qs0) << p.fold_log2) + BQ - 1) / BQ) * g_item, p.n_split, p.part_steps);
+          ok = part < n_parts;
+        }
       }
     } else if (ok) {
       ok = s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end &&
@@ -1179,7 +1197,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
 
       const int qb_start = CROSS ? 0 : (k0_in / BQ) * BQ;
       const int nqb = (s_len - qb_start + BQ - 1) / BQ;
-      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, p.n_split) : StepRange{0, nqb * g_item};
+      const StepRange range = CROSS ? part_of_steps((int64_t)nqb * g_item, part, n_parts) : StepRange{0, nqb * g_item};
       const int n_steps = range.to - range.from;
       const int w_share = quotient(n_resident, min(p.Hkv * p.n_split, kNumXcd * kHeadGroup));
       const int set = quotient(tl.tile, max(w_share, 1));
@@ -1453,7 +1471,7 @@ __device__ __forceinline__ void dkdv8_items(int block, int n_resident) {
           }
       };
       auto store = [&](const f32x16 (&acc)[NDB], uint16_t* out, int64_t st, int64_t sh, float* parts, float scale) {
-        if (p.n_split == 1) {
+        if (n_parts == 1) {
           if (wave_active) {  // through what this wave alone has read
             const uint32_t at = theirs - lane * 16;
             RowStage<DQK>::put(at, lane, acc, scale);
@@ -1522,10 +1540,18 @@ __global__ __launch_bounds__(2 * kThreads, 2) void bwd_both_kernel(const BwdPara
 // 2 (32/4) 112 -> 60, 5.6; T = 4096, 4 parts: 97 -> 10.  Four loads of a thread are under way from five parts
 // on; with fewer a thread waits for each of its one to three, and the many workgroups make up for it.
 constexpr int kReduceUnits = 2;
-template <int DQK, int DV>
+// CROSS: T and cu are those of the keys, Tk and cu_kv of the query rows, and an item has as many parts as the key-tile kernel gave it: one is no sum.
+template <int DQK, int DV, bool CROSS = false>
 __global__ __launch_bounds__(kThreads) void bwd_reduce_parts_kernel(const BwdParams p) {
   const hbp_tile tl = p.tiles[blockIdx.x];
   if (tl.sample < 0 || tl.sample >= p.n_samples) return;
+  int n_split = p.n_split;
+  if constexpr (CROSS) {
+    const int qs0 = p.cu_kv[tl.sample], qs1 = p.cu_kv[tl.sample + 1];
+    if (!(0 <= qs0 && qs0 <= qs1 && qs1 <= p.Tk)) return;
+    n_split = parts_of_steps((int64_t)((((qs1 - qs0) << p.fold_log2) + 63) / 64) * p.g, p.n_split, p.part_steps);
+    if (n_split == 1 && DQK == DV) return;  // has its sums; at head size 192 they are here all the same (see dkdv_items)
+  }
   const int s0 = p.cu[tl.sample], s1 = p.cu[tl.sample + 1];
   if (!(s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
         tl.row_end - tl.row_begin <= 128))
@@ -1542,14 +1568,14 @@ __global__ __launch_bounds__(kThreads) void bwd_reduce_parts_kernel(const BwdPar
     const int64_t part_stride = (int64_t)p.T * p.Hkv * dim;
     f32x4 acc = *(const f32x4*)src;
     int part = 1;
-    for (; part + 4 <= p.n_split; part += 4) {  // four loads under way
+    for (; part + 4 <= n_split; part += 4) {  // four loads under way
       f32x4 v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = *(const f32x4*)(src + (part + i) * part_stride);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc += v[i];
     }
-    for (; part < p.n_split; ++part) acc += *(const f32x4*)(src + part * part_stride);
+    for (; part < n_split; ++part) acc += *(const f32x4*)(src + part * part_stride);
     uint16_t* dst = is_k ? p.dk + key * p.k_st + (int64_t)kh * p.k_sh + x : p.dv + key * p.v_st + (int64_t)kh * p.v_sh + x;
     *(u32x2*)dst = u32x2{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3])};
   }
@@ -1794,16 +1820,18 @@ __global__ __launch_bounds__(kThreads) void cross_reduce_dq_kernel(const BwdPara
   if (!(s0 >= 0 && s1 <= p.T && s0 <= tl.row_begin && tl.row_begin < tl.row_end && tl.row_end <= s1 &&
         tl.row_end - tl.row_begin <= 256 >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk))
     return;
+  const int parts = key_parts(ks1 - ks0, p.dq_parts, p.dq_part_keys).n;
+  if (parts == 1) return;  // has its dQ
   const int n_units = ((tl.row_end - tl.row_begin) << p.fold_log2) * LPR;
   const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
   for (int u = blockIdx.y * kThreads + threadIdx.x; u < n_units; u += gridDim.y * kThreads) {
     const int f = u / LPR, x = u - f * LPR;
     const float* src = p.dq_part + (row0 + f) * DQK + 4 * x;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int at = 0; at < p.dq_parts; at += 8) {  // eight parts' loads under way
+    for (int at = 0; at < parts; at += 8) {  // eight parts' loads under way
       f32x4 v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = at + i < p.dq_parts ? *(const f32x4*)(src + (at + i) * rows * DQK) : f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 8; ++i) v[i] = at + i < parts ? *(const f32x4*)(src + (at + i) * rows * DQK) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc += v[i];
     }
@@ -1844,7 +1872,7 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     else both = cross_both_four_kernel<DQK, DV>;
     if (const int err = raise_lds_limit((const void*)both, lds, both_done)) return err;
     hipLaunchKernelGGL(both, dim3((unsigned)(n_dkdv + n_dq)), dim3(kEight ? 2 * kThreads : kThreads), lds, s, p, (int)n_dkdv, (int)n_dq,
-                       (int)cross_dq_first(p.T, p.Tk, (p.Hq / p.Hkv), p.n_split, p.dq_parts));
+                       p.dq_first);
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
@@ -1860,8 +1888,10 @@ static int launch_cross_bwd_t(const BwdParams& p, hipStream_t s) {
     BwdParams keys = p;  // the reduce kernel's rows are the keys
     keys.T = p.Tk;
     keys.cu = p.cu_kv;
+    keys.cu_kv = p.cu;
+    keys.Tk = p.T;
     const int units = 128 * p.Hkv * ((DQK + DV) / 4), share = kThreads * kReduceUnits;
-    hipLaunchKernelGGL((bwd_reduce_parts_kernel<DQK, DV>), dim3(p.n_tiles, (units + share - 1) / share), dim3(kThreads), 0, s, keys);
+    hipLaunchKernelGGL((bwd_reduce_parts_kernel<DQK, DV, true>), dim3(p.n_tiles, (units + share - 1) / share), dim3(kThreads), 0, s, keys);
     e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }

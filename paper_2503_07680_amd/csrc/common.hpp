@@ -245,8 +245,14 @@ struct Fold {
   }
 };
 
-// Keys of a part, where a sample's n keys are dealt out in `parts` at most, of `least` at least; whole key tiles.
-__device__ __forceinline__ int keys_of_a_part(int n, int parts, int least) { return (max((n + parts - 1) / parts, least) + 63) / 64 * 64; }
+// A sample's n keys dealt out in `most` parts at most, of `least` keys at least; whole key tiles.
+struct KeyParts {
+  int keys, n;  // of a part, and how many there are: one where there are no keys
+};
+__device__ __forceinline__ KeyParts key_parts(int n, int most, int least) {
+  const int keys = (max(max((n + most - 1) / most, least), 1) + 63) / 64 * 64;
+  return {keys, __builtin_amdgcn_readfirstlane(max((n + keys - 1) / keys, 1))};
+}
 
 // Tile copy with the lane-dependent part (LDS row, swizzled chunk) packed once per kernel.  Rows
 // >= rows_valid re-read the last valid row (never out of bounds; the caller masks their products).
@@ -820,7 +826,9 @@ struct BwdParams {
   // steps over the query rows (see cross_dkdv).
   const int32_t* cu_kv;
   int32_t Tk, fold_log2;
-  int32_t dq_parts;  // a sample's keys are dealt out in so many for dQ; from two on:
+  int32_t part_steps;              // of a part, at least; 0: every item is dealt out in n_split
+  int32_t dq_first;                // in a common launch
+  int32_t dq_part_keys, dq_parts;  // a sample's keys are dealt out for dQ in so many parts at most, of dq_part_keys at least; from two on:
   float* dq_part;    // [part][folded group][token][F][d_qk]
 };
 

@@ -111,17 +111,57 @@ inline CrossFwdLayout cross_fwd_layout(const hbp_cross_desc& d) {
   return l;
 }
 
+// A workgroup's fair share of the backward, in dK/dV's steps (64 rows of a head, 128 keys): one of dQ, 256 rows and 64 keys, is 1.5 of
+// them.  By the mean lengths with their tiles' empty rows, or by the pairs of rows and keys, where long samples are long on both sides.
+inline int64_t cross_bwd_share(const hbp_cross_desc& d) {
+  const CrossTiles t = cross_tiles(d);
+  const int64_t items = ((int64_t)d.total_keys + kCrossKeys - 1) / kCrossKeys * d.n_kv_heads;
+  const int64_t steps = (int64_t)d.total_queries * (d.n_q_heads / d.n_kv_heads) / d.n_samples / 64;
+  const int64_t by_mean = (2 * items * steps + 3 * t.items * t.key_tiles) / 2 / 256;
+  const int64_t by_pairs = d.pairs / (64 * kCrossKeys) * d.n_q_heads / 256 * 7 / 4;
+  return by_mean > by_pairs ? by_mean : by_pairs;
+}
+// Whether an item of so many of dK/dV's steps (some 1.1 us each) holds up the launch by more than its parts cost, of which most have
+// nothing to do (a workgroup 2 us) where few samples are long: then the share is the length of a part.  Backward, us, by the mean -> here
+// (* on a card that is 4 % slower): one sample of 8000 queries and 200 keys, 30 of 100 and 100, 32/8 heads of 128: 674 -> 218*, 8/1: 210 -> 108*;
+// 20000 and 1500, 24 of 500 and 1500, 8/1: 3267 -> 1227*, 12/3 of 64: 1141 -> 595*; 10 and 30000, 30 of 100 and 100, 32/8: 486 -> 157*,
+// 24 heads: 569 -> 365*; 300 and 4000, 11 of 300 and 300, 8/1: 122 -> 67*; 16 samples log-normal with a spread of 1, 8/1: 732 -> 447*.
+// Without the parts' cost in the rule 8000 and 200 with 24 heads went from 196 to 268*, 300 and 4000 from 146 to 164*.
+inline bool cross_holds_up(int64_t steps, int64_t share, int64_t workgroups) { return steps > 64 + workgroups / 32 && steps > 2 * share; }
+// At head size 192 dQ's items are halves of a tile, and an item of dK/dV that is one part goes through the workspace too.
+inline int64_t cross_items_cost(const hbp_cross_desc& d) { return d.d_qk > 128 ? 2 : 1; }
+constexpr int64_t kCrossMostParts = 16;  // of a long sample: the workspace has room for as many of every one
+struct CrossBwdParts {
+  int parts, least;  // at most, for one item; steps or keys of a part at least
+};
+inline CrossBwdParts cross_dkdv_parts(const hbp_cross_desc& d) {
+  const int parts = cross_parts(d);
+  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return {parts, 0};
+  const int64_t longest = (int64_t)(d.longest_queries < d.total_queries ? d.longest_queries : d.total_queries) * (d.n_q_heads / d.n_kv_heads) / 64;
+  const int64_t share = cross_bwd_share(d), least = share < 32 ? 32 : share;
+  int64_t more = (longest + least - 1) / least;
+  if (more > kCrossMostParts) more = kCrossMostParts;
+  if (!cross_holds_up(longest / parts, share, ((int64_t)d.total_keys + kCrossKeys - 1) / kCrossKeys * d.n_kv_heads * more * cross_items_cost(d))) return {parts, 0};
+  return {(int)more, (int)least};
+}
+
 // The same for dQ, beside dK/dV in one launch.  In products of 64-column blocks: an item of dQ takes 3 x 256 rows x its keys, all
 // of dQ that times its items, all of dK/dV 4 x rows x keys.  An item that is longer than a compute unit's share of the two is cut.
 // Backward, us, in one part -> as here: 118 queries, 7467 keys, 32/8 heads of 128: 172 -> 69; 74, 5994, 6/2 of 64: 73 -> 22.5; 34,
 // 5300, 8/1: 109 -> 24; 112, 5400, 12/3: 117 -> 31; 52, 4222, 24: 103 -> 50.  (By the forward's rule 16 samples of 450 queries and
 // 800 keys, 8/1 heads, went from 132 to 167.)
-inline int cross_dq_parts(const hbp_cross_desc& d) {
-  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return 1;
+inline CrossBwdParts cross_dq_parts(const hbp_cross_desc& d) {
+  if (d.total_keys == 0 || d.total_queries == 0 || d.n_samples == 0) return {1, 0};
   const CrossTiles t = cross_tiles(d);
   int64_t parts = 256 * 3 * kCrossRows / (t.items * 3 * kCrossRows + (int64_t)d.total_queries * d.n_q_heads * 4);
   if (parts > t.key_tiles / 2) parts = t.key_tiles / 2;
-  return (int)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+  parts = parts < 1 ? 1 : parts > 32 ? 32 : parts;
+  const int64_t longest = ((int64_t)(d.longest_keys < d.total_keys ? d.longest_keys : d.total_keys) + 63) / 64;
+  const int64_t share = cross_bwd_share(d), least = share < 32 ? 21 : share * 2 / 3;
+  int64_t more = (longest + least - 1) / least;
+  if (more > kCrossMostParts) more = kCrossMostParts;
+  if (!cross_holds_up(longest * 3 / 2 / parts, share, t.items * more * cross_items_cost(d))) return {(int)parts, 0};
+  return {(int)more, (int)(least * 64)};
 }
 
 // Workgroups that share the rows of a tile where parts are added up: some 1024 in all, and no more than a tile has work for.
@@ -130,31 +170,39 @@ inline int cross_join_shares(int groups, int tiles) {
   return n < 4 ? 4 : n > 32 ? 32 : (int)n;
 }
 
-// Whether the items of dQ are longer than those of dK/dV in the mean: a step over 64 keys costs one of dQ's 256 rows three
-// products, a step over 64 rows one of dK/dV's 128 keys four.
-inline bool cross_dq_first(int64_t queries, int64_t keys, int group, int parts, int dq_parts) {
-  return keys * 3 * 256 / dq_parts > queries * group * 4 * 128 / parts;
-}
-
 // dK/dV and dQ in one launch, a workgroup an item, as long as the items' numbers stay exact in the kernel's quotients.  Against two
 // launches, 77 packs of 40 to 19600 tokens a side, 4/4 to 128/128 heads: 1.1 to 1.6 where the launches have few rounds, 1.0 to 1.1 in
 // large packs, .99 at worst.
 inline bool cross_one_launch(int64_t n_dkdv, int64_t n_dq) { return n_dkdv > 0 && n_dq > 0 && n_dkdv + n_dq < (1 << 22); }
 
+// Whether dQ's items come before those of dK/dV: those that are longer, in the mean, or, where long samples have parts of their own, at most.
+inline bool cross_dq_first(const hbp_cross_desc& d, const CrossBwdParts& dkdv, const CrossBwdParts& dq) {
+  const int64_t group = d.n_q_heads / d.n_kv_heads;
+  if (dkdv.least == 0 && dq.least == 0) return (int64_t)d.total_keys * 3 * 256 / dq.parts > d.total_queries * group * 4 * 128 / dkdv.parts;
+  const int64_t steps = dkdv.least ? dkdv.least : d.longest_queries * group / 64 / dkdv.parts;
+  const int64_t tiles = dq.least ? dq.least / 64 : d.longest_keys / 64 / dq.parts;
+  return 3 * tiles > 2 * steps;
+}
+
 struct CrossBwdLayout {
   size_t d_off, lse2_off, dk_part_off, dv_part_off, dq_part_off, total;
-  int parts, dq_parts;
+  int parts, part_steps, dq_parts, dq_part_keys;
+  bool dq_first;
 };
 inline CrossBwdLayout cross_bwd_layout(const hbp_cross_desc& d) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   CrossBwdLayout l;
-  l.parts = cross_parts(d);
+  const CrossBwdParts dkdv = cross_dkdv_parts(d), dq = cross_dq_parts(d);
+  l.parts = dkdv.parts;
+  l.part_steps = dkdv.least;
   const size_t rows = up((size_t)d.n_q_heads * d.total_queries * 4), sums = l.parts > 1 ? (size_t)l.parts * d.total_keys * d.n_kv_heads * 4 : 0;
   l.d_off = 0;
   l.lse2_off = rows;
   l.dk_part_off = 2 * rows;
   l.dv_part_off = l.dk_part_off + up(sums * d.d_qk);
-  l.dq_parts = cross_dq_parts(d);
+  l.dq_parts = dq.parts;
+  l.dq_part_keys = dq.least;
+  l.dq_first = cross_dq_first(d, dkdv, dq);
   l.dq_part_off = l.dv_part_off + up(sums * d.d_v);
   l.total = l.dq_part_off + (l.dq_parts > 1 ? up((size_t)l.dq_parts * d.n_q_heads * d.total_queries * d.d_qk * 4) : 0);
   return l;

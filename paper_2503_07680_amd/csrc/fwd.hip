@@ -397,7 +397,7 @@ __device__ __forceinline__ void fwd_items() {
     const int halves = HP * TP == 1 ? p.halves : 0, half = __builtin_popcount(tile_idx) & halves;
     hbp_tile tl;
     int s0, s1;
-    int ks0 = 0, ks1 = 0;
+    int ks0 = 0, ks1 = 0, n_parts = 1;
     bool ok;
     if constexpr (CROSS) ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.cu_kv, p.n_samples, lane, tl, s0, s1, ks0, ks1);
     else ok = load_tile(p.tiles, tile_idx >> halves, p.cu, p.n_samples, lane, tl, s0, s1);
@@ -408,10 +408,11 @@ __device__ __forceinline__ void fwd_items() {
              BM * half < (tl.row_end - tl.row_begin) << p.fold_log2;
         if (ok && p.parts > 1) {  // this workgroup's part of the keys
           static_assert(BN == 64, "a part is whole key tiles");
-          const int n = ks1 - ks0, per = keys_of_a_part(n, p.parts, p.part_keys), from = min((int64_t)per * blockIdx.y, (int64_t)n);
-          ok = from < n || blockIdx.y == 0;
-          ks1 = min(n - from, per) + ks0 + from;
-          ks0 += from;
+          const KeyParts of = key_parts(ks1 - ks0, p.parts, p.part_keys);
+          n_parts = of.n;
+          ok = (int)blockIdx.y < n_parts;
+          ks0 += ok ? of.keys * (int)blockIdx.y : 0;
+          ks1 = min((int64_t)ks0 + of.keys, (int64_t)ks1);
         }
       }
     } else if (ok) {
@@ -614,7 +615,7 @@ __device__ __forceinline__ void fwd_items() {
         const bool row_valid = l32 < rows_left;
         if constexpr (CROSS) {
           const int f0 = r0 + 32 * rw, f = f0 + l32;
-          if (p.parts > 1) {
+          if (n_parts > 1) {
             const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2;
             const int64_t row = blockIdx.y * rows + (((int64_t)h * p.T + tl.row_begin) << p.fold_log2) + f;
             if (row_valid) {
@@ -706,7 +707,8 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p)
         tl.row_end - tl.row_begin <= 256 >> p.fold_log2 && 0 <= ks0 && ks0 <= ks1 && ks1 <= p.Tk))
     return;
   const int n_rows = (tl.row_end - tl.row_begin) << p.fold_log2, x = threadIdx.x % LPR;
-  const int per = max(keys_of_a_part(ks1 - ks0, p.parts, p.part_keys), 64), parts = max((int)(((int64_t)ks1 - ks0 + per - 1) / per), 1);
+  const int parts = key_parts(ks1 - ks0, p.parts, p.part_keys).n;
+  if (parts == 1) return;  // has its O
   const int64_t rows = (int64_t)p.Hkv * p.g * p.T << p.fold_log2, row0 = ((int64_t)blockIdx.x * p.T + tl.row_begin) << p.fold_log2;
   for (int f = blockIdx.y * (kThreads / LPR) + threadIdx.x / LPR; f < n_rows; f += gridDim.y * (kThreads / LPR)) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -722,7 +724,7 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(const FwdParams p)
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (at + i >= parts || ml[i][0] == -INFINITY) continue;  // a sample without keys
+        if (at + i >= parts) continue;
         const float top = fmaxf(m, ml[i][0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[i][0] - top);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = acc[j] * a + o[i][j] * b;

@@ -179,12 +179,14 @@ class PackedCrossAttention:
         self.desc = B.CrossDesc(total_queries=self.Tq, total_keys=self.Tk, n_samples=len(q_lengths),
                                 n_q_heads=self.Hq, n_kv_heads=self.Hkv, d_qk=self.d_qk, d_v=self.d_v,
                                 softmax_scale=float(softmax_scale),
-                                longest_keys=max((int(k) for q, k in zip(q_lengths, kv_lengths) if q), default=0))
+                                longest_keys=max((int(k) for q, k in zip(q_lengths, kv_lengths) if q), default=0),
+                                longest_queries=max((int(q) for q, k in zip(q_lengths, kv_lengths) if k), default=0))
         self.cu_q, self.cu_kv, q_tiles, self.pairs = B.hbp_cross_plan(
             q_lengths, kv_lengths, B.hbp_cross_tile_rows(self.desc, B.HBP_FWD), B.HBP_TILES_QUERY)
         _, _, kv_tiles, _ = B.hbp_cross_plan(
             q_lengths, kv_lengths, B.hbp_cross_tile_rows(self.desc, B.HBP_BWD), B.HBP_TILES_KEY)
         self.n_q_tiles, self.n_kv_tiles = len(q_tiles), len(kv_tiles)
+        self.desc.pairs = self.pairs
         # one copy; 16 bytes a tile, so both lists start on a tile's alignment
         plan = torch.from_numpy(np.concatenate([q_tiles.ravel(), kv_tiles.ravel(), self.cu_q, self.cu_kv])).to(self.device)
         self.q_tiles_dev, self.kv_tiles_dev, self.cu_q_dev, self.cu_kv_dev = plan.split(

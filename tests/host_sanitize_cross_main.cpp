@@ -66,14 +66,18 @@ int main() {
     d.n_kv_heads = 1 + (int32_t)(rnd() % 64);
     d.n_q_heads = d.n_kv_heads * (1 + (int32_t)(rnd() % 64));
     d.longest_keys = rnd() % 2 ? 0 : size_up_to(31);
+    d.longest_queries = rnd() % 2 ? 0 : size_up_to(31);
+    d.pairs = rnd() % 2 ? 0 : (int64_t)size_up_to(31) * size_up_to(31);
     d.d_qk = dims[round % 3][0];
     d.d_v = dims[round % 3][1];
-    const int fold = hbp::cross_fold_log2(d), parts = hbp::cross_parts(d), dq = hbp::cross_dq_parts(d);
+    const int fold = hbp::cross_fold_log2(d), parts = hbp::cross_parts(d), dq = hbp::cross_dq_parts(d).parts;
     const hbp::CrossFwdParts f_parts = hbp::cross_fwd_parts(d);
     const int fwd = f_parts.parts;
     CHECK(f_parts.keys >= 0 && f_parts.keys % 64 == 0 && (f_parts.keys == 0 || (d.longest_keys > 0 && fwd > 1 && f_parts.keys < INT_MAX - 4096)));
     CHECK(fold >= 0 && fold <= 5 && (d.n_q_heads / d.n_kv_heads) % (1 << fold) == 0);
     CHECK(parts >= 1 && parts <= 32 && fwd >= 1 && fwd <= 32 && dq >= 1 && dq <= 32);
+    const hbp::CrossBwdParts dkdv = hbp::cross_dkdv_parts(d);
+    CHECK(dkdv.parts >= 1 && dkdv.parts <= 32 && dkdv.least >= 0);
     const hbp::CrossFwdLayout f = hbp::cross_fwd_layout(d);
     const hbp::CrossBwdLayout b = hbp::cross_bwd_layout(d);
     CHECK(f.total % 256 == 0 && b.total % 256 == 0 && f.o_off <= f.ml_off && f.ml_off <= f.total);
@@ -81,7 +85,6 @@ int main() {
     CHECK(b.d_off <= b.lse2_off && b.lse2_off <= b.dk_part_off && b.dk_part_off <= b.dv_part_off && b.dv_part_off <= b.dq_part_off && b.dq_part_off <= b.total);
     const int shares = hbp::cross_join_shares(d.n_q_heads >> fold, 1 + (int)(rnd() % 30000));
     CHECK(shares >= 4 && shares <= 32);
-    (void)hbp::cross_dq_first(d.total_queries, d.total_keys, d.n_q_heads / d.n_kv_heads, parts, dq);
   }
   std::printf("ok\n");
   return 0;
