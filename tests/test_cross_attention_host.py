@@ -137,5 +137,17 @@ def test_the_longest_sample_goes_into_the_workspace():
     assert need[0] == need[1756] == need[3000] == 0 and need[50000] > 0
     all_keys, more = (H.hbp_cross_workspace_bytes(H.CrossDesc(longest_keys=k, **kw), H.HBP_FWD) for k in (56200, 2 ** 31 - 1))
     assert all_keys == more >= need[50000]
-    with pytest.raises(H.HbpError):
-        H.hbp_cross_workspace_bytes(H.CrossDesc(longest_keys=-1, **kw), H.HBP_FWD)
+    for field in ("longest_keys", "longest_queries", "pairs"):
+        with pytest.raises(H.HbpError):
+            H.hbp_cross_workspace_bytes(H.CrossDesc(**{field: -1}, **kw), H.HBP_FWD)
+
+
+def test_long_samples_go_into_the_backwards_workspace():
+    """Long query runs on few keys, and long keys under few queries, have parts of their own; samples long on both sides do not."""
+    kw = dict(total_queries=11000, total_keys=11000, n_samples=31, n_q_heads=32, n_kv_heads=8, d_qk=128, d_v=128)
+
+    def need(**more):
+        return H.hbp_cross_workspace_bytes(H.CrossDesc(**kw, **more), H.HBP_BWD)
+
+    assert need(longest_queries=8000, longest_keys=200, pairs=8000 * 100 + 30 * 100 * 360) > need() < need(longest_keys=10000, pairs=2000000)
+    assert need(longest_queries=8000, longest_keys=8000, pairs=8000 * 8000 + 30 * 100 * 100) == need() == need(longest_queries=500, longest_keys=500)
