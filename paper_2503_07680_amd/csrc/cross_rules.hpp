@@ -122,11 +122,11 @@ inline int64_t cross_bwd_share(const hbp_cross_desc& d) {
   return by_mean > by_pairs ? by_mean : by_pairs;
 }
 // Whether an item of so many of dK/dV's steps (some 1.1 us each) holds up the launch by more than its parts cost, of which most have
-// nothing to do (a workgroup 2 us) where few samples are long: then the share is the length of a part.  Backward, us, by the mean -> here
-// (* on a card that is 4 % slower): one sample of 8000 queries and 200 keys, 30 of 100 and 100, 32/8 heads of 128: 674 -> 218*, 8/1: 210 -> 108*;
-// 20000 and 1500, 24 of 500 and 1500, 8/1: 3267 -> 1227*, 12/3 of 64: 1141 -> 595*; 10 and 30000, 30 of 100 and 100, 32/8: 486 -> 157*,
-// 24 heads: 569 -> 365*; 300 and 4000, 11 of 300 and 300, 8/1: 122 -> 67*; 16 samples log-normal with a spread of 1, 8/1: 732 -> 447*.
-// Without the parts' cost in the rule 8000 and 200 with 24 heads went from 196 to 268*, 300 and 4000 from 146 to 164*.
+// nothing to do (a workgroup 2 us) where few samples are long: then the share is the length of a part.  Backward, us, by the mean -> here:
+// one sample of 8000 queries and 200 keys, 30 of 100 and 100, 32/8 heads of 128: 673 -> 212, 8/1: 210 -> 108; 20000 and 1500, 24 of 500 and
+// 1500, 8/1: 3277 -> 1217, 12/3 of 64: 1142 -> 566; 10 and 30000, 30 of 100 and 100, 32/8: 484 -> 157, 24 heads: 565 -> 364; 300 and 4000,
+// 11 of 300 and 300, 8/1: 121 -> 64; 16 samples log-normal with a spread of 1, 8/1: 735 -> 432.  Without the parts' cost in the rule 8000
+// and 200 with 24 heads went from 196 to 265, 300 and 4000 from 146 to 161.
 inline bool cross_holds_up(int64_t steps, int64_t share, int64_t workgroups) { return steps > 64 + workgroups / 32 && steps > 2 * share; }
 // At head size 192 dQ's items are halves of a tile, and an item of dK/dV that is one part goes through the workspace too.
 inline int64_t cross_items_cost(const hbp_cross_desc& d) { return d.d_qk > 128 ? 2 : 1; }
